@@ -452,7 +452,7 @@ def exact(case, seed):
         wg = (w * grad.reshape(w.shape)).sum(3)
         w = w.sum(3)
         total = w.sum(2)
-        c = torch.where(total > 0, w[:, :, 1] / total, 0.0)
-        # d mix_j / d z = mix_j (1 - c) on the right of the node, -mix_j c on its left
-        out[rows, (1 << m) - 1:(2 << m) - 1] = wg[:, :, 1] * (1 - c) - wg[:, :, 0] * c
+        # d mix_j / d z = mix_j (1 - c) on the right of the node, -mix_j c on its left; c the right half's share, 1 - c the left half's
+        left, right = (torch.where(total > 0, w[:, :, k] / total, 0.0) for k in (0, 1))
+        out[rows, (1 << m) - 1:(2 << m) - 1] = wg[:, :, 1] * left - wg[:, :, 0] * right
     return dict(dlogits=out)
