@@ -126,6 +126,44 @@ fff_status_t fff_create_w8(fff_handle_t *out, int D, int O, int depth, int leaf_
                            const uint8_t *leaf_w2_e4m3, const float *leaf_w2_scale, const void *leaf_b2);
 
 /*
+ * The same layer with its leaf weights stored as microscaled 4-bit floats (as fff_quantize_mx4 makes them): rows of e2m1 codes,
+ * two per byte, the even column in the low half, and one e8m0 scale per block of 32 columns.
+ *
+ *   leaf_w1_e2m1   [2^d, l, (D + 1) / 2]     leaf_w1_scale  [2^d, l, (D + 31) / 32]
+ *   leaf_w2_e2m1   [2^d, l, (O + 1) / 2]     leaf_w2_scale  [2^d, l, (O + 31) / 32]      W2 TRANSPOSED: the O weights that leave a
+ *                                                            hidden unit are a row (leaves are thin: blocks along l would be
+ *                                                            mostly scales)
+ *
+ * A weight is the value of its code times 2^(scale - 127), exactly; a block with scale 255 is NaN, a product too large for bfloat16
+ * infinite.  Everything else (x, y, node weights, biases) is bfloat16; products are accumulated in float32, hidden values keep
+ * float32 precision to 2^-18.  (The paper stores its weights in one floating-point type; this takes 17/64 of bfloat16's bytes.)
+ * Any D, O and depth; FFF_ERR_UNSUPPORTED for l > 1024.  fff_forward_train is not available on such a handle, and it stays on
+ * FFF_PATH_AUTO.  The caller's arrays are read while the call runs and not kept.
+ */
+fff_status_t fff_create_mx4(fff_handle_t *out, int D, int O, int depth, int leaf_width, fff_activation_t act,
+                            const void *node_w, const void *node_b,
+                            const uint8_t *leaf_w1_e2m1, const uint8_t *leaf_w1_scale, const void *leaf_b1,
+                            const uint8_t *leaf_w2_e2m1, const uint8_t *leaf_w2_scale, const void *leaf_b2);
+
+/*
+ * Conversion of rows of numbers to microscaled 4-bit floats and back (OCP Microscaling Formats 1.0, MXFP4; the paper has no
+ * counterpart).  A block is 32 neighbouring columns of a row (the last one may be shorter); its scale is 2^(floor(log2 a) - 2) for
+ * its largest magnitude a, 2^-127 at least; every element divided by the scale is rounded to the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6
+ * and their negatives, ties to the even code, more than 6 to 6.  A block with an infinity or a NaN becomes NaN (scale 255, codes 0).
+ *
+ *   src      [rows, cols]  in, float32 or bfloat16 (dtype)
+ *   codes    [rows, (cols + 1) / 2]     out / in: the even column in the low half; the upper half of an odd row's last byte is 0
+ *   scales   [rows, (cols + 31) / 32]   out / in: biased exponents
+ *   values   [rows, cols]  the numbers that the codes stand for, in dtype; out of fff_quantize_mx4 too, where it may be NULL
+ *
+ * The calls use the current device, keep no state and only enqueue one kernel.  rows or cols 0: FFF_OK, nothing is written.
+ */
+fff_status_t fff_quantize_mx4(const void *src, fff_dtype_t dtype, int64_t rows, int64_t cols, uint8_t *codes, uint8_t *scales,
+                              void *values, void *cuda_stream);
+fff_status_t fff_dequantize_mx4(const uint8_t *codes, const uint8_t *scales, fff_dtype_t dtype, int64_t rows, int64_t cols, void *values,
+                                void *cuda_stream);
+
+/*
  * FORWARD_I of Algorithm 1 for B tokens, enqueued on `cuda_stream`.
  *
  *   x         [B, D]  in
@@ -168,6 +206,55 @@ fff_status_t fff_forward_infer(fff_handle_t h, const void *x, void *y, int32_t *
  */
 fff_status_t fff_forward_train(fff_handle_t h, const void *x, void *y, float *mixture, float *node_entropy,
                                int64_t B, void *cuda_stream);
+
+/*
+ * The balance loss of a batch's routing: whether the leaves share its tokens.  (The paper names the problem, leaves that
+ * few tokens reach, and has no loss for it; the form is the usual one of mixtures of experts.)
+ * A token counts if its mask is not 0 and its leaf is in [0, 2^d).  With n tokens that count, f_j the share of them routed to leaf j
+ * and P_j the mean of their mixture weights of leaf j:
+ *     loss = 2^d sum_j f_j P_j          (1 where both are even; 0 with n = 0)
+ *
+ *   mixture       [B, 2^d]  in, float32: the weights of fff_forward_train
+ *   leaf_idx      [B]       in: the leaves of fff_tree_descent or fff_forward_infer
+ *   token_mask    [B]       in, bytes, may be NULL: 0 leaves a token (padding) out, whatever its row holds
+ *   loss          [1]       out, may be NULL
+ *   counts        [2^d]     out, may be NULL: tokens of every leaf
+ *   mean_mixture  [2^d]     out, may be NULL: P
+ *
+ * Enqueues one kernel; allocates nothing.  Sums are added in a fixed order (float32 over a few hundred tokens, float64 above).
+ * Uses scratch of the handle, like every call: one at a time.
+ */
+fff_status_t fff_balance_loss(fff_handle_t h, const float *mixture, const int32_t *leaf_idx, const uint8_t *token_mask, float *loss,
+                              int32_t *counts, float *mean_mixture, int64_t B, void *cuda_stream);
+
+/*
+ * Its gradient with respect to the mixture weights: dmixture[b, j] = dloss 2^d f_j / n for a token that counts, 0 for the others.
+ * (Counts carry no gradient.)
+ *
+ *   leaf_idx, token_mask    as above; leaf_idx may be NULL where every token has a leaf
+ *   counts     [2^d]        in: of fff_balance_loss, or their sum over the processes that share a batch; f = counts / n, n = their sum
+ *   dloss      [1]          in: the gradient of the loss, in device memory
+ *   dmixture   [B, 2^d]     out
+ */
+fff_status_t fff_balance_loss_backward(fff_handle_t h, const int32_t *leaf_idx, const uint8_t *token_mask, const int32_t *counts,
+                                       const float *dloss, float *dmixture, int64_t B, void *cuda_stream);
+
+/*
+ * From the mixture weights back to the node logits z = <w, x> + b.  With g_j = dmixture[b, j] (plus the balance loss's gradient), and M and S
+ * the sums of mixture_j and mixture_j g_j over the leaves of a child, every node gets
+ *     dlogits = S_right (1 - c) - S_left c,    c = M_right / (M_left + M_right)
+ * and 0 where both children's weights are too small for float32 (below 2^-126).  The gradients of a node's parameters and of x follow
+ * as dlogits^T x, sums of dlogits, and dlogits node_w.
+ *
+ *   mixture      [B, 2^d]       in
+ *   dmixture     [B, 2^d]       in, may be NULL where counts and dloss are given
+ *   counts, dloss               in, both or neither: adds the gradient of the balance loss without its matrix; leaf_idx (may be NULL) as above
+ *   token_mask   [B]            in, may be NULL: the rows of masked tokens become 0, whatever they hold
+ *   dlogits      [B, 2^d - 1]   out, rows dense, nodes in the order of node_w.  Nothing is written for depth 0
+ */
+fff_status_t fff_routing_backward(fff_handle_t h, const float *mixture, const float *dmixture, const int32_t *leaf_idx,
+                                  const uint8_t *token_mask, const int32_t *counts, const float *dloss, float *dlogits, int64_t B,
+                                  void *cuda_stream);
 
 /*
  * The same computation for buffers in HOST memory (pinned or pageable):

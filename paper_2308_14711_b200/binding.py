@@ -10,6 +10,7 @@ shape and contiguity, and passes their data_ptr().
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -26,7 +27,8 @@ TUNING = {"tcgen05_descent": 0, "tcgen05_grouped": 1, "tcgen05_leaf": 2, "cta_pa
           "token_blocks": 7}
 
 # every symbol include/fff.h declares
-EXPORTS = ["fff_create", "fff_create_w8", "fff_forward_infer", "fff_forward_train", "fff_forward_infer_host", "fff_destroy", "fff_reserve",
+EXPORTS = ["fff_create", "fff_create_w8", "fff_create_mx4", "fff_quantize_mx4", "fff_dequantize_mx4", "fff_balance_loss",
+           "fff_balance_loss_backward", "fff_routing_backward", "fff_forward_infer", "fff_forward_train", "fff_forward_infer_host", "fff_destroy", "fff_reserve",
            "fff_set_path", "fff_set_tuning", "fff_tree_descent", "fff_leaf_bucketing", "fff_grouped_leaf_ff",
            "fff_debug_get_bucketing", "fff_get_last_status", "fff_capabilities", "fff_selftest_bounded_wait", "fff_last_launch_count", "fff_status_string",
            "fff_profile_begin", "fff_profile_end", "fff_profile_launches", "fff_profile_launch_name",
@@ -61,6 +63,12 @@ def lib():
     L.fff_set_path.argtypes = [vp, ci]
     L.fff_set_tuning.argtypes = [vp, ci, ci]
     L.fff_create_w8.argtypes = [C.POINTER(vp), ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.fff_create_mx4.argtypes = [C.POINTER(vp), ci, ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.fff_quantize_mx4.argtypes = [vp, ci, i64, i64, vp, vp, vp, vp]
+    L.fff_dequantize_mx4.argtypes = [vp, vp, ci, i64, i64, vp, vp]
+    L.fff_balance_loss.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    L.fff_balance_loss_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, vp]
+    L.fff_routing_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     L.fff_capabilities.argtypes = [vp]
     L.fff_forward_train.argtypes = [vp, vp, vp, vp, vp, i64, vp]
     L.fff_stack_create.argtypes = [C.POINTER(vp), ci, C.POINTER(vp), ci, C.POINTER(vp), C.POINTER(vp), C.c_float, ci]
@@ -225,6 +233,63 @@ def _stream_ptr(stream=None):
     return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
+def _stream_of(t, stream):
+    """cudaStream_t of `stream`, by default the current stream of the tensor's device."""
+    return stream.cuda_stream if stream is not None else _torch()._C._cuda_getCurrentRawStream(t.device.index)
+
+
+def _on_device(t):
+    """Makes the tensor's device the current one (nothing to do where it is)."""
+    torch = _torch()
+    return contextlib.nullcontext() if t.device.index == torch._C._cuda_getDevice() else torch.cuda.device(t.device)
+
+
+def _mask_ptr(mask, B):
+    """Bytes that are 0 for the tokens to leave out: a bool or uint8 tensor."""
+    torch = _torch()
+    return _ptr(mask, torch.bool if mask is not None and mask.dtype == torch.bool else torch.uint8, (B,), "token_mask")
+
+
+def _mx4_dtype(dtype):
+    torch = _torch()
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"4-bit conversion takes float32 or bfloat16, got {dtype}")
+    return DTYPES["f32" if dtype == torch.float32 else "bf16"]
+
+
+def quantize_mx4(w, want_values: bool = False, stream=None):
+    """Microscaled 4-bit floats of the rows (last dimension) of a float32 or bfloat16 tensor: returns (codes, scales), or
+    (codes, scales, values) with the numbers that the codes stand for in w's type.  codes uint8 [..., (cols + 1) // 2], two per byte,
+    scales uint8 [..., (cols + 31) // 32]."""
+    torch = _torch()
+    if w.dim() < 1:
+        raise ValueError("w: expected rows")
+    cols, lead = w.shape[-1], tuple(w.shape[:-1])
+    dtype, wp = _mx4_dtype(w.dtype), _ptr(w, w.dtype, w.shape, "w")
+    codes = torch.empty(lead + ((cols + 1) // 2,), dtype=torch.uint8, device=w.device)
+    scales = torch.empty(lead + ((cols + 31) // 32,), dtype=torch.uint8, device=w.device)
+    values = torch.empty_like(w, memory_format=torch.contiguous_format) if want_values else None
+    with _on_device(w):
+        _check(lib().fff_quantize_mx4(wp, dtype, w.numel() // max(cols, 1), cols, codes.data_ptr(), scales.data_ptr(),
+                                      None if values is None else values.data_ptr(), _stream_of(w, stream)), "fff_quantize_mx4")
+    return (codes, scales, values) if want_values else (codes, scales)
+
+
+def dequantize_mx4(codes, scales, cols: int, dtype=None, stream=None):
+    """The numbers that codes and scales (of rows of `cols` columns) stand for, bfloat16 unless dtype is torch.float32."""
+    torch = _torch()
+    dtype = torch.bfloat16 if dtype is None else dtype
+    lead = tuple(codes.shape[:-1])
+    d = _mx4_dtype(dtype)
+    cp = _ptr(codes, torch.uint8, lead + ((cols + 1) // 2,), "codes")
+    sp = _ptr(scales, torch.uint8, lead + ((cols + 31) // 32,), "scales")
+    values = torch.empty(lead + (cols,), dtype=dtype, device=codes.device)
+    with _on_device(codes):
+        _check(lib().fff_dequantize_mx4(cp, sp, d, values.numel() // max(cols, 1), cols, values.data_ptr(), _stream_of(codes, stream)),
+               "fff_dequantize_mx4")
+    return values
+
+
 class FFFLayer:
     """One FFF layer on the current CUDA device; tensors in, tensors out, all work in libfff.so."""
 
@@ -253,11 +318,38 @@ class FFFLayer:
                                  _ptr(node_w, td, (nn, D), "node_w"), _ptr(node_b, td, (nn,), "node_b"),
                                  _ptr(w1, td, (nl, leaf_width, D), "w1"), _ptr(b1, td, (nl, leaf_width), "b1"),
                                  _ptr(w2, td, (nl, O, leaf_width), "w2"), _ptr(b2, td, (nl, O), "b2"))
-        self._bf16 = self.tdtype == torch.bfloat16
-        call = torch_call()
-        self._forward = call.forward if call is not None else lambda *args: None
+        self._bind_forward()
         if path != "auto":
             self.set_path(path)
+
+    def _bind_forward(self) -> None:
+        self._bf16 = self.tdtype == _torch().bfloat16
+        call = torch_call()
+        self._forward = call.forward if call is not None else lambda *args: None
+
+    @classmethod
+    def from_mx4(cls, D: int, O: int, depth: int, leaf_width: int, activation: str, node_w, node_b, w1_codes, w1_scales, b1, w2_codes,
+                 w2_scales, b2) -> "FFFLayer":
+        """A layer with microscaled 4-bit leaf weights (fff_create_mx4), as quantize_mx4 makes them of w1 [2^d, l, D] and of w2
+        TRANSPOSED to [2^d, l, O]; everything else bfloat16."""
+        torch = _torch()
+        self = cls.__new__(cls)
+        self._h = None
+        self.D, self.O, self.depth, self.l = D, O, depth, leaf_width
+        self.n_leaves = 1 << depth
+        self.tdtype = td = torch.bfloat16
+        nl, u8 = self.n_leaves, torch.uint8
+        out = C.c_void_p()
+        _check(lib().fff_create_mx4(C.byref(out), D, O, depth, leaf_width, ACTIVATIONS[activation],
+                                    _ptr(node_w, td, (nl - 1, D), "node_w"), _ptr(node_b, td, (nl - 1,), "node_b"),
+                                    _ptr(w1_codes, u8, (nl, leaf_width, (D + 1) // 2), "w1 codes"),
+                                    _ptr(w1_scales, u8, (nl, leaf_width, (D + 31) // 32), "w1 scales"), _ptr(b1, td, (nl, leaf_width), "b1"),
+                                    _ptr(w2_codes, u8, (nl, leaf_width, (O + 1) // 2), "w2 codes"),
+                                    _ptr(w2_scales, u8, (nl, leaf_width, (O + 31) // 32), "w2 scales"), _ptr(b2, td, (nl, O), "b2")),
+               "fff_create_mx4")
+        self._h = out.value
+        self._bind_forward()
+        return self
 
     @property
     def handle(self) -> int:
@@ -324,6 +416,44 @@ class FFFLayer:
                                        None if mix is None else mix.data_ptr(), None if ent is None else ent.data_ptr(), B,
                                        self._stream(stream)), "fff_forward_train")
         return y, mix, (None if ent is None else ent[:self.n_leaves - 1])
+
+    def balance_loss(self, mixture, leaf_idx, token_mask=None, stream=None):
+        """The balance loss of a batch (mixture [B, 2^d] float32 of forward_train, leaf_idx [B] int32, token_mask [B] bool or uint8, False or
+        0 for tokens to leave out): returns (loss float32, counts int32 [2^d], mean mixture weights float32 [2^d])."""
+        torch = _torch()
+        B, dev = mixture.shape[0], mixture.device
+        mp, lp = _ptr(mixture, torch.float32, (B, self.n_leaves), "mixture"), _ptr(leaf_idx, torch.int32, (B,), "leaf_idx")
+        loss = torch.empty((), dtype=torch.float32, device=dev)
+        counts = torch.empty((self.n_leaves,), dtype=torch.int32, device=dev)
+        mean = torch.empty((self.n_leaves,), dtype=torch.float32, device=dev)
+        _check(lib().fff_balance_loss(self._h, mp, lp, _mask_ptr(token_mask, B), loss.data_ptr(), counts.data_ptr(), mean.data_ptr(), B,
+                                      _stream_of(mixture, stream)), "fff_balance_loss")
+        return loss, counts, mean
+
+    def balance_loss_backward(self, leaf_idx, counts, dloss, token_mask=None, stream=None):
+        """Gradient of the balance loss with respect to the mixture weights, float32 [B, 2^d]; dloss: one float32 on the device."""
+        torch = _torch()
+        B = leaf_idx.shape[0]
+        lp, cp = _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"), _ptr(counts, torch.int32, (self.n_leaves,), "counts")
+        gp = _ptr(dloss, torch.float32, dloss.shape if dloss.numel() == 1 else (1,), "dloss")
+        out = torch.empty((B, self.n_leaves), dtype=torch.float32, device=leaf_idx.device)
+        _check(lib().fff_balance_loss_backward(self._h, lp, _mask_ptr(token_mask, B), cp, gp, out.data_ptr(), B, _stream_of(leaf_idx, stream)),
+               "fff_balance_loss_backward")
+        return out
+
+    def routing_backward(self, mixture, dmixture=None, leaf_idx=None, counts=None, dloss=None, token_mask=None, stream=None):
+        """Gradient with respect to the node logits, float32 [B, 2^d - 1], of a loss with gradient dmixture [B, 2^d] (may be None) plus, where
+        counts and dloss are given, of the balance loss."""
+        torch = _torch()
+        B = mixture.shape[0]
+        f32 = torch.float32
+        mp, dp = _ptr(mixture, f32, (B, self.n_leaves), "mixture"), _ptr(dmixture, f32, (B, self.n_leaves), "dmixture")
+        lp, cp = _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"), _ptr(counts, torch.int32, (self.n_leaves,), "counts")
+        gp = None if dloss is None else _ptr(dloss, f32, dloss.shape if dloss.numel() == 1 else (1,), "dloss")
+        out = torch.empty((B, self.n_leaves - 1), dtype=f32, device=mixture.device)
+        _check(lib().fff_routing_backward(self._h, mp, dp, lp, _mask_ptr(token_mask, B), cp, gp, out.data_ptr(), B, _stream_of(mixture, stream)),
+               "fff_routing_backward")
+        return out
 
     def forward_infer_host(self, x_host, y_host, leaf_idx_host=None, stream=None) -> None:
         """x_host / y_host / leaf_idx_host: contiguous CPU tensors (pinned for full copy speed)."""

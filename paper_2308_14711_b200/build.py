@@ -18,7 +18,7 @@ CALL_SRC = os.path.join(CSRC, "torch_call.cpp")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-         "-Xcompiler", "-fPIC,-Wall", "-shared", "--expt-relaxed-constexpr"]
+         "-Xcompiler", "-fPIC,-Wall", "-shared", "--expt-relaxed-constexpr", "--threads", "0"]
 
 
 def sources():
@@ -26,7 +26,7 @@ def sources():
 
 
 def _deps():
-    return sources() + glob.glob(os.path.join(CSRC, "**", "*.cuh"), recursive=True) + \
+    return sources() + glob.glob(os.path.join(CSRC, "**", "*.cuh"), recursive=True) + glob.glob(os.path.join(CSRC, "*.h")) + \
         glob.glob(os.path.join(os.path.dirname(HERE), "include", "*.h"))
 
 

@@ -30,6 +30,7 @@
 #include "kernels/leaf_warp.cuh"
 #include "kernels/stack.cuh"
 #include "kernels/token_block.cuh"
+#include "launch.h"
 
 namespace {
 
@@ -72,6 +73,10 @@ struct fff_handle_s {
     bool w8 = false;
     unsigned char *w1codes = nullptr, *w2codes = nullptr;
     float *scale1 = nullptr, *scale2 = nullptr;
+    // microscaled 4-bit leaf weights (fff_create_mx4): the images of mx4.cu
+    bool mx4 = false;
+    fff::Mx4Layer mx;
+    void* bal_scratch = nullptr;       // of the balance loss (routing.cu); its size depends on the number of leaves alone
     // grouped tiles of the tcgen05 leaf kernel (8 leaves per tile, bins = the nodes three levels above the leaves):
     // weight images (nullptr = shapes not eligible) and the first stage that ends at those nodes
     __nv_bfloat16* g_w1 = nullptr;
@@ -289,6 +294,7 @@ void prof_free(fff_handle_s* h) {
 
 void release(fff_handle_s* h) {
     dfree(h->w2t);
+    dfree(h->mx.w1); dfree(h->mx.w2); dfree(h->mx.s1); dfree(h->mx.s2); dfree(h->bal_scratch);
     dfree(h->node_w); dfree(h->node_b); dfree(h->w1); dfree(h->b1); dfree(h->w2); dfree(h->b2);
     dfree(h->ws_leaf); dfree(h->ws_perm); dfree(h->ws_perm2); dfree(h->ws_offsets); dfree(h->ws_offsets2[0]); dfree(h->ws_offsets2[1]);
     dfree(h->d_status); dfree(h->st_x); dfree(h->st_y); dfree(h->st_leaf);
@@ -375,8 +381,15 @@ int leaf_mma_slots(const fff_handle_s* h, int tile_rows) {
     }
 }
 
+// Rows of a tile of the 4-bit leaf kernel: 64 where leaves have them and enough tiles are left for two CTAs per SM (a leaf's weights are
+// expanded once per 32 rows and once per tile), as long as the hidden values of a tile fit beside another CTA's.
+int mx4_tile_rows(const fff_handle_s* h, int64_t B) {
+    return h->l <= 128 && B > 32 * h->n_leaves && expected_tiles(h, B, 64) >= 2.0 * h->sm_count ? 64 : 32;
+}
+
 LeafPlan leaf_plan(const fff_handle_s* h, int64_t B) {
     if (h->w8) return LeafPlan{fff::kLUM, true};
+    if (h->mx4) return LeafPlan{mx4_tile_rows(h, B), false};
     // While the tiles of all leaves are resident at once, the mma.sync kernel (two CTAs per SM for leaves of up to 32 neurons,
     // no tensor memory to set up) is ahead: 768 -> 768, 256 leaves of 12, with the descent: 19.3 against 24.1 us at 4096 tokens
     // and 19.6 against 24.6 at 6144 (32-row tiles), 22.7 against 25.8 at 8192 and 25.0 against 30.1 at 12 608 (64-row tiles);
@@ -409,6 +422,7 @@ bool warp_tiles(const fff_handle_s* h, const LeafPlan& plan, int64_t B) {
 
 bool use_tensor_leaf(const fff_handle_s* h) {
     if (h->w8) return true;            // 8-bit leaf weights exist for the tcgen05 leaf kernel only
+    if (h->mx4) return h->mx.mma;
     if (h->LP == 0 || h->path == FFF_PATH_WARP) return false;
     return h->path == FFF_PATH_TENSOR || h->l >= 8;
 }
@@ -462,7 +476,7 @@ fff_status_t grow_workspace(fff_handle_s* h, int64_t B) {
     // kMaxSlotBytes the forward keeps the bucketing kernel instead.  k_block_forward has no other way: for the layers that
     // run it the table stops growing there, and larger batches go through it in parts.
     const bool filed_by_descent = !h->ustages.empty() && h->ustages.back().umma &&
-                                  h->ustages.back().L0 + h->ustages.back().k == h->depth && (h->w2uimg || h->w2codes);
+                                  h->ustages.back().L0 + h->ustages.back().k == h->depth && (h->w2uimg || h->w2codes || h->mx.mma);
     const int64_t most = listed_tokens(h);
     if (runs_block_forward(h) || ((filed_by_descent || (h->bf_per_sm > 0 && h->bf_pinnable)) && B <= most)) {
         int64_t cap = std::min(B, most);
@@ -1041,6 +1055,29 @@ fff_status_t pack_node_images(fff_handle_s* h) {
     return cudaGetLastError() == cudaSuccess ? FFF_OK : FFF_ERR_CUDA;
 }
 
+fff::LaunchOn launch_on_handle(const fff_handle_s* h, cudaStream_t st) {
+    return fff::LaunchOn{st, h->device, h->sm_count, h->pdl && !h->prof_active};
+}
+
+// Layers with 4-bit leaf weights: thin leaves, a warp per token.
+fff_status_t run_leaf_mx4_rows(fff_handle_s* h, const void* x, const int32_t* leaf_idx, const int32_t* perm, void* y, int64_t B,
+                               cudaStream_t st, const DescentTail& tail, int32_t* leaf_out) {
+    const fff::Mx4Tail walk{h->node_w, h->node_b, tail.level0, tail.levels, tail.pos, leaf_out};
+    if (fff::mx4_leaf_rows(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->b1, h->b2, h->act}, leaf_idx, perm, B, walk) != cudaSuccess)
+        return cudaGetLastError(), FFF_ERR_CUDA;
+    return launched(h, st, tail.levels > 0 ? "descent_tail+leaf_ff_mx4_rows" : "grouped_leaf_ff_mx4_rows");
+}
+
+// ... and the others, on tiles of a leaf's tokens.
+fff_status_t run_leaf_mx4(fff_handle_s* h, const void* x, const int32_t* perm, void* y, int64_t B, int tile_rows, cudaStream_t st) {
+    // direct lists: perm is the table of lists, the tiles come from its counts
+    int32_t* counts = h->slots_now && perm == h->ws_slots ? h->ws_cursor : nullptr;
+    if (fff::mx4_leaf_tiles(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->b1, h->b2, h->act}, perm, h->ws_tiles,
+                            tile_list_len(B, tile_rows, (int)h->n_leaves), tile_rows, counts, (int)h->n_leaves, (int)h->slot_cap) != cudaSuccess)
+        return cudaGetLastError(), FFF_ERR_CUDA;
+    return launched(h, st, "grouped_leaf_ff_mx4");
+}
+
 // Which form of k_leaf_warp: while the warps of all tokens are resident at once with the registers that the general form wants
 // (three CTAs per SM, four where the kernel walks the last levels too), that one; beyond, the loads of six CTAs per SM outweigh the
 // few that each has in flight, as long as the leaves are narrow and rows come in vectors (769 columns, 4096 leaves of 16, 12 000 tokens
@@ -1051,6 +1088,7 @@ fff_status_t pack_node_images(fff_handle_s* h) {
 template <typename T>
 fff_status_t run_leaf(fff_handle_s* h, const void* x, const int32_t* leaf_idx, const int32_t* perm, void* y,
                       int64_t B, cudaStream_t st, const DescentTail& tail = DescentTail(), int32_t* leaf_out = nullptr) {
+    if (h->mx4) return run_leaf_mx4_rows(h, x, leaf_idx, perm, y, B, st, tail, leaf_out);
     const int64_t blocks = std::min<int64_t>((B + fff::kLeafWarps - 1) / fff::kLeafWarps, (int64_t)h->sm_count * 8);
     const size_t smem = sizeof(float) * (size_t)fff::kLeafWarps * h->l;
     auto launch = [&](auto kern) {
@@ -1145,6 +1183,7 @@ fff_status_t launch_leaf_umma(fff_handle_s* h, const void* x, const int32_t* per
 fff_status_t run_leaf_mma(fff_handle_s* h, const void* x, const int32_t* perm, void* y, int64_t B, const LeafPlan& plan,
                           cudaStream_t st) {
     const int tile_rows = plan.tile_rows;
+    if (h->mx4) return run_leaf_mx4(h, x, perm, y, B, tile_rows, st);
     if (h->w8) {
         switch (h->LP) {
             case 16: return launch_leaf_umma<16, false, true>(h, x, perm, y, B, tile_rows, st);
@@ -1486,7 +1525,7 @@ fff_status_t run_block_forward(fff_handle_s* h, const void* x, void* y, int32_t*
 constexpr int64_t kTokenBlockMaxB = 512, kTokenBlockMaxBDeep = 2048, kTokenBlockMaxBytes = (int64_t)96 << 20;
 
 bool use_token_block(const fff_handle_s* h, int64_t B) {
-    if (h->w8 || h->path != FFF_PATH_AUTO || !h->tune[FFF_TUNE_TOKEN_BLOCKS]) return false;
+    if (h->w8 || h->mx4 || h->path != FFF_PATH_AUTO || !h->tune[FFF_TUNE_TOKEN_BLOCKS]) return false;
     if (fff::TokenBlockLayout{h->D, h->l, (int)h->esize}.total() > 100 * 1024) return false;
     const bool two_stages = use_tensor_leaf(h) && h->ustages.size() >= 2;
     if (two_stages) {
@@ -1825,11 +1864,34 @@ const char* fff_status_string(fff_status_t s) {
 
 namespace {
 
-// fff_create and fff_create_w8: w1_scale != nullptr means leaf_w1 / leaf_w2 are e4m3 codes with per-leaf scales.
+// The images of 4-bit leaf weights, from the caller's codes and scales.
+fff_status_t make_mx4_images(fff_handle_s* h, const uint8_t* w1, const uint8_t* s1, const uint8_t* w2, const uint8_t* s2) {
+    const int64_t nl = h->n_leaves, n1 = nl * h->l * ((h->D + 31) / 32), n2 = nl * h->l * ((h->O + 31) / 32);
+    h->mx.D = h->D; h->mx.O = h->O; h->mx.l = h->l;
+    h->mx.mma = fff::mx4_on_tensor_cores(h->l);
+    const fff::Mx4Bytes bytes = fff::mx4_image_bytes(h->mx, nl);
+    int* flag = nullptr;
+    int big = 0;
+    fff_status_t s = clone((void**)&flag, nullptr, sizeof(int));
+    if (s == FFF_OK && (fff::mx4_find_big(s1, n1, flag, h->sm_count) != cudaSuccess || fff::mx4_find_big(s2, n2, flag, h->sm_count) != cudaSuccess ||
+                        cudaMemcpy(&big, flag, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess))
+        s = (cudaGetLastError(), FFF_ERR_CUDA);
+    dfree(flag);
+    h->mx.big = big != 0;
+    if (s == FFF_OK) s = dmalloc((void**)&h->mx.w1, bytes.w1);
+    if (s == FFF_OK) s = dmalloc((void**)&h->mx.s1, bytes.s1);
+    if (s == FFF_OK) s = dmalloc((void**)&h->mx.w2, bytes.w2);
+    if (s == FFF_OK) s = dmalloc((void**)&h->mx.s2, bytes.s2);
+    if (s == FFF_OK && fff::mx4_pack(h->mx, w1, s1, w2, s2, nl, h->sm_count) != cudaSuccess) s = (cudaGetLastError(), FFF_ERR_CUDA);
+    return s;
+}
+
+// fff_create, fff_create_w8 and fff_create_mx4: w1_scale != nullptr means leaf_w1 / leaf_w2 are e4m3 codes with per-leaf scales,
+// w1_mx != nullptr that they are e2m1 codes with block scales.
 fff_status_t create_common(fff_handle_t* out, int D, int O, int depth, int leaf_width, fff_activation_t act,
                            fff_dtype_t dtype, const void* node_w, const void* node_b, const void* leaf_w1,
                            const void* leaf_b1, const void* leaf_w2, const void* leaf_b2, const float* w1_scale,
-                           const float* w2_scale) {
+                           const float* w2_scale, const uint8_t* w1_mx = nullptr, const uint8_t* w2_mx = nullptr) {
     if (!out) return FFF_ERR_INVALID_ARG;
     *out = nullptr;
     if (D < 1 || O < 1 || leaf_width < 1 || depth < 0) return FFF_ERR_INVALID_ARG;
@@ -1837,10 +1899,13 @@ fff_status_t create_common(fff_handle_t* out, int D, int O, int depth, int leaf_
     if (dtype != FFF_DTYPE_F32 && dtype != FFF_DTYPE_BF16) return FFF_ERR_INVALID_ARG;
     if (depth > FFF_MAX_DEPTH) return FFF_ERR_UNSUPPORTED;
     if (!leaf_w1 || !leaf_w2 || (depth > 0 && !node_w)) return FFF_ERR_INVALID_ARG;
-    for (const void* p : {node_w, node_b, leaf_w1, leaf_b1, leaf_w2, leaf_b2, (const void*)w1_scale, (const void*)w2_scale})
+    for (const void* p : {node_w, node_b, leaf_w1, leaf_b1, leaf_w2, leaf_b2, (const void*)w1_scale, (const void*)w2_scale, (const void*)w1_mx,
+                          (const void*)w2_mx})
         if (p && !aligned16(p)) return FFF_ERR_INVALID_ARG;
     const bool w8 = w1_scale != nullptr;
     if (w8 && (!w2_scale || dtype != FFF_DTYPE_BF16)) return FFF_ERR_INVALID_ARG;
+    const bool mx4 = w1_mx != nullptr, coded = w8 || mx4;
+    if (mx4 && leaf_width > fff::kMx4MaxLeafWidth) return FFF_ERR_UNSUPPORTED;
     // 8-bit leaf weights run on the tcgen05 leaf kernel only
     if (w8 && (D % fff::kKS != 0 || O % 16 != 0 || leaf_width > 64 || !encode_tiled_fn())) return FFF_ERR_UNSUPPORTED;
 
@@ -1880,14 +1945,16 @@ fff_status_t create_common(fff_handle_t* out, int D, int O, int depth, int leaf_
     if (s == FFF_OK) s = clone(&h->node_w, node_w, nn * D * e);
     if (s == FFF_OK) s = clone(&h->node_b, node_b, nn * e);
     h->w8 = w8;
-    if (s == FFF_OK && !w8) s = clone(&h->w1, leaf_w1, nl * leaf_width * D * e);
+    h->mx4 = mx4;
+    if (s == FFF_OK && !coded) s = clone(&h->w1, leaf_w1, nl * leaf_width * D * e);
     if (s == FFF_OK) s = clone(&h->b1, leaf_b1, nl * leaf_width * e);
-    if (s == FFF_OK && !w8) s = clone(&h->w2, leaf_w2, nl * O * leaf_width * e);
+    if (s == FFF_OK && !coded) s = clone(&h->w2, leaf_w2, nl * O * leaf_width * e);
     if (s == FFF_OK) s = clone(&h->b2, leaf_b2, nl * O * e);
     if (s == FFF_OK) s = clone((void**)&h->ws_offsets, nullptr, sizeof(int32_t) * (nl + 1));
     if (s == FFF_OK) s = clone((void**)&h->ws_offsets2[0], nullptr, sizeof(int32_t) * (nl + 1));
     if (s == FFF_OK) s = clone((void**)&h->ws_offsets2[1], nullptr, sizeof(int32_t) * (nl + 1));
     if (s == FFF_OK) s = clone((void**)&h->d_status, nullptr, sizeof(int));
+    if (s == FFF_OK) s = clone(&h->bal_scratch, nullptr, fff::balance_scratch_bytes(h->n_leaves));       // zeroed
     {
         int coop = 0, per_sm = 0;
         cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, h->device);
@@ -1922,14 +1989,16 @@ fff_status_t create_common(fff_handle_t* out, int D, int O, int depth, int leaf_
             fff::k_pack_b1<__nv_bfloat16><<<h->sm_count * 8, 256>>>((const __nv_bfloat16*)h->b1, h->b1img, (int)nl, leaf_width, LP);
             if (cudaGetLastError() != cudaSuccess) s = FFF_ERR_CUDA;
         }
+    } else if (s == FFF_OK && mx4) {
+        s = make_mx4_images(h, (const uint8_t*)leaf_w1, w1_mx, (const uint8_t*)leaf_w2, w2_mx);
     } else if (s == FFF_OK && dtype == FFF_DTYPE_BF16 && D % 8 == 0 && O % 8 == 0 && leaf_width <= 64) {
         h->LP = leaf_width <= 16 ? 16 : (leaf_width <= 32 ? 32 : 64);
         s = pack_leaf_images<__nv_bfloat16>(h);
     }
-    if (s == FFF_OK && !w8 && h->w2uimg) s = pack_group_images<__nv_bfloat16>(h);
-    if (s == FFF_OK && !w8) s = FFF_DISPATCH(h, plan_block_forward, h);
+    if (s == FFF_OK && !coded && h->w2uimg) s = pack_group_images<__nv_bfloat16>(h);
+    if (s == FFF_OK && !coded) s = FFF_DISPATCH(h, plan_block_forward, h);
     if (s == FFF_OK) s = plan_block_tiles(h);
-    if (s == FFF_OK && !w8) plan_train(h);
+    if (s == FFF_OK && !coded) plan_train(h);
     if (s == FFF_OK && cudaDeviceSynchronize() != cudaSuccess) s = (cudaGetLastError(), FFF_ERR_CUDA);
     if (s != FFF_OK) { release(h); return s; }
     {
@@ -1959,6 +2028,14 @@ fff_status_t fff_create_w8(fff_handle_t* out, int D, int O, int depth, int leaf_
                          leaf_b2, leaf_w1_scale, leaf_w2_scale);
 }
 
+fff_status_t fff_create_mx4(fff_handle_t* out, int D, int O, int depth, int leaf_width, fff_activation_t act, const void* node_w,
+                            const void* node_b, const uint8_t* leaf_w1_e2m1, const uint8_t* leaf_w1_scale, const void* leaf_b1,
+                            const uint8_t* leaf_w2_e2m1, const uint8_t* leaf_w2_scale, const void* leaf_b2) {
+    if (!leaf_w1_scale || !leaf_w2_scale) return out ? (*out = nullptr, FFF_ERR_INVALID_ARG) : FFF_ERR_INVALID_ARG;
+    return create_common(out, D, O, depth, leaf_width, act, FFF_DTYPE_BF16, node_w, node_b, leaf_w1_e2m1, leaf_b1, leaf_w2_e2m1,
+                         leaf_b2, nullptr, nullptr, leaf_w1_scale, leaf_w2_scale);
+}
+
 fff_status_t fff_destroy(fff_handle_t h) {
     {
         std::lock_guard<std::mutex> lk(g_mu);
@@ -1985,6 +2062,7 @@ fff_status_t fff_set_path(fff_handle_t h, fff_path_t path) {
     if (path == FFF_PATH_TENSOR && ((h->LP == 0 && h->stages.empty()) || h->D != h->Dp)) return FFF_ERR_UNSUPPORTED;
     if (path == FFF_PATH_FUSED && !h->bf_pinnable) return FFF_ERR_UNSUPPORTED;
     if (h->w8 && path != FFF_PATH_AUTO && path != FFF_PATH_TENSOR) return FFF_ERR_UNSUPPORTED;
+    if (h->mx4 && path != FFF_PATH_AUTO) return FFF_ERR_UNSUPPORTED;
     h->path = path;
     if (runs_block_forward(h) && h->cap_B > 0 && !h->ws_slots) {      // a workspace sized without its lists
         DeviceGuard g(h->device);
@@ -2173,6 +2251,110 @@ fff_status_t fff_forward_train(fff_handle_t h, const void* x, void* y, float* mi
     return run_forward_train(h, x, y, mixture, node_entropy, B, (cudaStream_t)cuda_stream);
 }
 
+// ---- routing losses
+
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+fff_status_t fff_balance_loss(fff_handle_t h, const float* mixture, const int32_t* leaf_idx, const uint8_t* token_mask, float* loss,
+                              int32_t* counts, float* mean_mixture, int64_t B, void* cuda_stream) {
+    fff_status_t s = check_forward_args(h, B);
+    if (s != FFF_OK) return s;
+    if (B > 0 && (!mixture || !leaf_idx || !aligned16(mixture))) return FFF_ERR_INVALID_ARG;
+    if (!aligned4(leaf_idx) || !aligned4(loss) || !aligned4(counts) || !aligned4(mean_mixture)) return FFF_ERR_INVALID_ARG;
+    h->launches = 0;
+    if (!loss && !counts && !mean_mixture) return FFF_OK;
+    DeviceGuard g(h->device);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (fff::balance_loss(launch_on_handle(h, st), mixture, leaf_idx, token_mask, loss, counts, mean_mixture, B, h->n_leaves, h->bal_scratch) !=
+        cudaSuccess)
+        return cudaGetLastError(), FFF_ERR_CUDA;
+    return launched(h, st, "balance_loss");
+}
+
+fff_status_t fff_balance_loss_backward(fff_handle_t h, const int32_t* leaf_idx, const uint8_t* token_mask, const int32_t* counts,
+                                       const float* dloss, float* dmixture, int64_t B, void* cuda_stream) {
+    fff_status_t s = check_forward_args(h, B);
+    if (s != FFF_OK) return s;
+    h->launches = 0;
+    if (B == 0) return FFF_OK;
+    if (!counts || !dloss || !dmixture || !aligned16(dmixture) || !aligned4(counts) || !aligned4(dloss) || !aligned4(leaf_idx))
+        return FFF_ERR_INVALID_ARG;
+    DeviceGuard g(h->device);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (fff::balance_loss_backward(launch_on_handle(h, st), leaf_idx, token_mask, counts, dloss, dmixture, B, h->n_leaves) != cudaSuccess)
+        return cudaGetLastError(), FFF_ERR_CUDA;
+    return launched(h, st, "balance_loss_backward");
+}
+
+fff_status_t fff_routing_backward(fff_handle_t h, const float* mixture, const float* dmixture, const int32_t* leaf_idx,
+                                  const uint8_t* token_mask, const int32_t* counts, const float* dloss, float* dlogits, int64_t B,
+                                  void* cuda_stream) {
+    fff_status_t s = check_forward_args(h, B);
+    if (s != FFF_OK) return s;
+    h->launches = 0;
+    if (B == 0) return FFF_OK;
+    if ((counts == nullptr) != (dloss == nullptr) || (!counts && !dmixture)) return FFF_ERR_INVALID_ARG;
+    if (h->depth == 0) return FFF_OK;
+    if (!mixture || !dlogits || !aligned16(mixture) || !aligned16(dmixture) || !aligned16(dlogits) || !aligned4(counts) || !aligned4(dloss) ||
+        !aligned4(leaf_idx))
+        return FFF_ERR_INVALID_ARG;
+    DeviceGuard g(h->device);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    int n = 0;
+    if (fff::routing_backward(launch_on_handle(h, st), mixture, dmixture, leaf_idx, token_mask, counts, dloss, dlogits, B, h->depth,
+                              fff::balance_scratch_slope(h->bal_scratch, h->n_leaves), &n) != cudaSuccess)
+        return cudaGetLastError(), FFF_ERR_CUDA;
+    h->launches = n;
+    return FFF_OK;
+}
+
+// ---- microscaled 4-bit conversion
+
+// The current device as the launchers want it.
+static fff_status_t current_device(fff::LaunchOn* on, void* cuda_stream) {
+    static std::mutex mu;
+    static int sms[kMaxDevices] = {};
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return cudaGetLastError(), FFF_ERR_CUDA;
+    if (dev < 0 || dev >= kMaxDevices) return FFF_ERR_UNSUPPORTED;
+    std::lock_guard<std::mutex> lk(mu);
+    if (sms[dev] == 0 && cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return sms[dev] = 0, cudaGetLastError(), FFF_ERR_CUDA;
+    *on = fff::LaunchOn{(cudaStream_t)cuda_stream, dev, sms[dev], true};
+    return FFF_OK;
+}
+
+static fff_status_t check_mx4_args(fff_dtype_t dtype, int64_t rows, int64_t cols) {
+    if (dtype != FFF_DTYPE_F32 && dtype != FFF_DTYPE_BF16) return FFF_ERR_INVALID_ARG;
+    if (rows < 0 || cols < 0) return FFF_ERR_INVALID_ARG;
+    if (rows > 0 && cols > ((int64_t)1 << 40) / rows) return FFF_ERR_UNSUPPORTED;
+    return FFF_OK;
+}
+
+fff_status_t fff_quantize_mx4(const void* src, fff_dtype_t dtype, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales,
+                              void* values, void* cuda_stream) {
+    fff_status_t s = check_mx4_args(dtype, rows, cols);
+    if (s != FFF_OK || rows == 0 || cols == 0) return s;
+    if (!src || !codes || !scales || !aligned16(src) || !aligned16(codes) || !aligned16(scales) || !aligned16(values)) return FFF_ERR_INVALID_ARG;
+    fff::LaunchOn on;
+    if ((s = current_device(&on, cuda_stream)) != FFF_OK) return s;
+    if (fff::quantize_mx4(on, src, dtype == FFF_DTYPE_F32 ? 4 : 2, rows, cols, codes, scales, values) != cudaSuccess)
+        return cudaGetLastError(), FFF_ERR_CUDA;
+    return FFF_OK;
+}
+
+fff_status_t fff_dequantize_mx4(const uint8_t* codes, const uint8_t* scales, fff_dtype_t dtype, int64_t rows, int64_t cols, void* values,
+                                void* cuda_stream) {
+    fff_status_t s = check_mx4_args(dtype, rows, cols);
+    if (s != FFF_OK || rows == 0 || cols == 0) return s;
+    if (!codes || !scales || !values || !aligned16(codes) || !aligned16(scales) || !aligned16(values)) return FFF_ERR_INVALID_ARG;
+    fff::LaunchOn on;
+    if ((s = current_device(&on, cuda_stream)) != FFF_OK) return s;
+    if (fff::dequantize_mx4(on, codes, scales, dtype == FFF_DTYPE_F32 ? 4 : 2, rows, cols, values) != cudaSuccess)
+        return cudaGetLastError(), FFF_ERR_CUDA;
+    return FFF_OK;
+}
+
 // Chunks of a host-buffer forward: of 8192 tokens, or two for a smaller batch of at least 4 MB of x and y (less, and the
 // second chunk's submission and launches cost what the overlap saves), as long as the weights that a chunk fetches again cost
 // less than a quarter of its copies (16 times its bytes: memory is about 120 times as fast as the link).  One chunk against
@@ -2339,9 +2521,9 @@ int fff_capabilities(fff_handle_t h) {
     if (h->D == h->Dp) {
         if (!h->stages.empty() || !h->ustages.empty()) caps |= FFF_CAP_TENSOR_DESCENT;
         if (!h->ustages.empty()) caps |= FFF_CAP_TCGEN05_DESCENT;
-        if (h->LP != 0) caps |= FFF_CAP_TENSOR_LEAF;
+        if (h->LP != 0 || h->mx.mma) caps |= FFF_CAP_TENSOR_LEAF;
         if (h->w2uimg || h->w2codes) caps |= FFF_CAP_TCGEN05_LEAF;
-    } else if (!h->ustages.empty() || h->LP != 0) {
+    } else if (!h->ustages.empty() || h->LP != 0 || h->mx.mma) {
         caps |= FFF_CAP_PADDED;
     }
     if (h->bf_pinnable) caps |= FFF_CAP_FUSED_SMALL;

@@ -1,0 +1,448 @@
+// The balance loss of a batch's routing, and the gradients of losses on the mixture weights.
+//
+// A token b has mixture weights mix[b, j] over the L = 2^d leaves (FORWARD_T) and the leaf that FORWARD_I gives it.  Over the n
+// tokens that count (mask not zero, leaf in range):
+//     counts_j = tokens of leaf j,   f_j = counts_j / n,   P_j = mean of mix[., j],   loss = L sum_j f_j P_j,
+// smallest (1) where the leaves share tokens and weight evenly.  f is a count and carries no gradient:
+//     d loss / d mix[b, j] = L f_j / n  for a token that counts, 0 otherwise.
+// From the mixture weights back to the node logits: with g_j = d loss / d mix_j, and M and S the sums of mix_j and mix_j g_j over the
+// leaves below a child, the node's choice is c = M_right / (M_left + M_right) and
+//     d loss / d z = sum_j g_j d mix_j / d z = S_right (1 - c) - S_left c,
+// which needs no logits: one pass over the mixture weights, bottom-up.
+//
+// All three are bound by HBM: 4 B L bytes are read (twice that with a second gradient) or written, a few operations each.
+#pragma once
+
+#include <float.h>
+
+#include "common.cuh"
+
+namespace fff {
+
+// ---- balance loss ----------------------------------------------------------------------------------
+
+constexpr int kBalThreads = 1024;
+constexpr int kBalCols = 256;                 // columns (leaves) per tile
+constexpr int kBalMaxSlices = 296;            // row slices per tile when one tile has all columns: two CTAs per SM
+
+struct BalanceScratch {
+    float* sums;            // [slices][L]
+    int32_t* counts;        // [slices][L]
+    int32_t* rows;          // [tiles][slices] tokens that count
+    double* loss;           // [tiles] sum of counts_j * (sum of mix_j)
+    int* done;              // [tiles] + [1], zero between calls
+};
+
+__device__ __forceinline__ bool token_counts(const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask, int64_t b, int n_leaves, int& leaf) {
+    leaf = __ldg(leaf_idx + b);
+    return (unsigned)leaf < (unsigned)n_leaves && (!mask || __ldg(mask + b) != 0);
+}
+
+// Grid (slices, tiles).  Every CTA adds up its rows of its columns and counts its rows' leaves among them; the last CTA of a tile
+// adds up the slices in their order, the last tile the tiles: one launch, and the same bits every time.
+// V: columns per thread (4; 1 for one or two leaves).  Rows are added in float32 (at most a few hundred each), slices in float64.
+// 65 536 tokens, 2048 leaves (537 MB): measured in the table of routing losses; rows of one tile are 1 KB apart reads of 1 KB.
+template <int V>
+__global__ void __launch_bounds__(kBalThreads, 2)
+k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask,
+               float* __restrict__ loss, int32_t* __restrict__ counts, float* __restrict__ mean, int64_t B, int n_leaves,
+               BalanceScratch ws)
+{
+    constexpr int U = 4;                                  // rows whose loads are in flight
+    __shared__ int s_hist[kBalCols];
+    __shared__ float s_sum[kBalThreads * V], s_part[kBalThreads];
+    __shared__ double s_loss[kBalThreads / 32];
+    __shared__ int s_rows, s_last;
+    const int tid = threadIdx.x;
+    const int cols = min(n_leaves, kBalCols), col0 = blockIdx.y * cols;
+    const int across = cols / V, down = kBalThreads / across;            // threads per row, rows at a time (powers of two)
+    const int c = tid & (across - 1), r = tid / across;
+    const int slices = gridDim.x, tiles = gridDim.y;
+    const int64_t per = (B + slices - 1) / slices, b0 = blockIdx.x * per, b1 = min(B, b0 + per);
+    for (int i = tid; i < cols; i += kBalThreads) s_hist[i] = 0;
+    if (tid == 0) s_rows = 0;
+    __syncthreads();
+    pdl_trigger();
+    pdl_wait();
+
+    float acc[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) acc[v] = 0.0f;
+    int mine = 0;
+    const float* base = mix + col0 + c * V;
+    for (int64_t b = b0 + r; b < b1; b += (int64_t)U * down) {
+        float m[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = b + (int64_t)u * down;
+#pragma unroll
+            for (int v = 0; v < V; ++v) m[u][v] = 0.0f;
+            if (row >= b1) continue;
+            if constexpr (V == 4) {
+                const float4 q = __ldcs(reinterpret_cast<const float4*>(base + row * n_leaves));
+                m[u][0] = q.x; m[u][1] = q.y; m[u][2] = q.z; m[u][3] = q.w;
+            } else {
+                m[u][0] = __ldcs(base + row * n_leaves);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = b + (int64_t)u * down;
+            int leaf;
+            // (rows that do not count are left out, not multiplied by zero: they may hold anything)
+            if (row >= b1 || !token_counts(leaf_idx, mask, row, n_leaves, leaf)) continue;
+#pragma unroll
+            for (int v = 0; v < V; ++v) acc[v] += m[u][v];
+            if (c == 0) {
+                ++mine;
+                if ((unsigned)(leaf - col0) < (unsigned)cols) atomicAdd(&s_hist[leaf - col0], 1);
+            }
+        }
+    }
+    if (mine) atomicAdd(&s_rows, mine);
+#pragma unroll
+    for (int v = 0; v < V; ++v) s_sum[(r * across + c) * V + v] = acc[v];          // [down][cols]
+    __syncthreads();
+    // V rows per thread, the lanes of a warp that have the same column, then at most 32 partial sums per column
+    const int i = tid & (cols - 1), r2 = tid / cols;
+    const int parts = cols < 32 ? kBalThreads / 32 : kBalThreads / cols;
+    {
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) sum += s_sum[(r2 * V + v) * cols + i];
+        for (int o = cols; o < 32; o <<= 1) sum += __shfl_xor_sync(kFullMask, sum, o);
+        if (cols >= 32 || (tid & 31) < cols) s_part[(cols < 32 ? tid >> 5 : r2) * cols + i] = sum;
+    }
+    __syncthreads();
+    if (tid < cols) {
+        float sum = 0.0f;
+        for (int k = 0; k < parts; ++k) sum += s_part[k * cols + i];
+        ws.sums[(int64_t)blockIdx.x * n_leaves + col0 + i] = sum;
+        ws.counts[(int64_t)blockIdx.x * n_leaves + col0 + i] = s_hist[i];
+    }
+    if (tid == 0) ws.rows[blockIdx.y * slices + blockIdx.x] = s_rows;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) s_last = atomicAdd(ws.done + blockIdx.y, 1) == slices - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+
+    // ---- the tile's last CTA: several threads per column, then one
+    if (tid == 0) { s_rows = 0; ws.done[blockIdx.y] = 0; }
+    __syncthreads();
+    int rows = 0;
+    for (int s = tid; s < slices; s += kBalThreads) rows += __ldcg(ws.rows + blockIdx.y * slices + s);
+    if (rows) atomicAdd(&s_rows, rows);
+    const int down2 = kBalThreads / cols;
+    double sum = 0.0;
+    int cnt = 0;
+#pragma unroll 4
+    for (int s = r2; s < slices; s += down2) {
+        sum += (double)__ldcg(ws.sums + (int64_t)s * n_leaves + col0 + i);
+        cnt += __ldcg(ws.counts + (int64_t)s * n_leaves + col0 + i);
+    }
+    __shared__ double s_col[kBalThreads];
+    __shared__ int s_cnt[kBalThreads];
+    s_col[tid] = sum;
+    s_cnt[tid] = cnt;
+    __syncthreads();
+    const double n = (double)s_rows;
+    double part = 0.0;
+    if (tid < cols) {
+        for (int k = 1; k < min(down2, slices); ++k) {
+            sum += s_col[k * cols + i];
+            cnt += s_cnt[k * cols + i];
+        }
+        if (counts) counts[col0 + i] = cnt;
+        if (mean) mean[col0 + i] = n > 0.0 ? (float)(sum / n) : 0.0f;
+        part = (double)cnt * sum;
+        if (cnt == 0) part = 0.0;                         // (0 times a sum that overflowed)
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) part += __shfl_down_sync(kFullMask, part, o);
+    if ((tid & 31) == 0) s_loss[tid >> 5] = part;
+    __syncthreads();
+    if (tid == 0) {
+        double t = 0.0;
+        for (int w = 0; w < kBalThreads / 32; ++w) t += s_loss[w];
+        ws.loss[blockIdx.y] = t;
+        __threadfence();
+        s_last = atomicAdd(ws.done + tiles, 1) == tiles - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    double total = 0.0;
+    for (int t = tid; t < tiles; t += kBalThreads) total += __ldcg(ws.loss + t);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_down_sync(kFullMask, total, o);
+    __syncthreads();
+    if ((tid & 31) == 0) s_loss[tid >> 5] = total;
+    __syncthreads();
+    if (tid == 0) {
+        double t = 0.0;
+        for (int w = 0; w < kBalThreads / 32; ++w) t += s_loss[w];
+        if (loss) loss[0] = n > 0.0 ? (float)((double)n_leaves * t / (n * n)) : 0.0f;
+        ws.done[tiles] = 0;
+    }
+}
+
+// ---- its gradient ----------------------------------------------------------------------------------
+
+constexpr int kSlopeThreads = 512;
+
+// Tokens that count: the sum of the counts (all of which belong to such tokens).  By all threads of a CTA.
+__device__ __forceinline__ double counted_tokens(const int32_t* __restrict__ counts, int n_leaves, double* s_red) {
+    const int tid = threadIdx.x;
+    double n = 0.0;
+#pragma unroll 4
+    for (int j = tid; j < n_leaves; j += blockDim.x) n += (double)__ldg(counts + j);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFullMask, n, o);
+    if ((tid & 31) == 0) s_red[tid >> 5] = n;
+    __syncthreads();
+    n = 0.0;
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) n += s_red[w];      // (whole numbers: exact in any order)
+    __syncthreads();
+    return n;
+}
+
+// Grid (slices, tiles) as above; every thread keeps the slope of its columns and writes it (or zero) into its rows.
+template <int V>
+__global__ void __launch_bounds__(kSlopeThreads, 4)
+k_balance_loss_backward(const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask, const int32_t* __restrict__ counts,
+                        const float* __restrict__ dloss, float* __restrict__ dmix, int64_t B, int n_leaves)
+{
+    constexpr int U = 4;
+    __shared__ double s_red[kSlopeThreads / 32];
+    const int tid = threadIdx.x;
+    const int cols = min(n_leaves, kBalCols), col0 = blockIdx.y * cols;
+    const int across = cols / V, down = kSlopeThreads / across;
+    const int c = tid & (across - 1), r = tid / across;
+    pdl_trigger();
+    pdl_wait();
+    const double n = counted_tokens(counts, n_leaves, s_red);
+    const double scale = n > 0.0 ? (double)__ldg(dloss) * (double)n_leaves / (n * n) : 0.0;
+    float slope[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) slope[v] = (float)(scale * (double)__ldg(counts + col0 + c * V + v));
+    const int64_t per = (B + gridDim.x - 1) / gridDim.x, b0 = blockIdx.x * per, b1 = min(B, b0 + per);
+    float* base = dmix + col0 + c * V;
+    for (int64_t b = b0 + r; b < b1; b += (int64_t)U * down) {
+        bool in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = b + (int64_t)u * down;
+            int leaf;
+            in[u] = row < b1 && (leaf_idx ? token_counts(leaf_idx, mask, row, n_leaves, leaf) : (!mask || __ldg(mask + row) != 0));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = b + (int64_t)u * down;
+            if (row >= b1) break;
+            if constexpr (V == 4)
+                __stcs(reinterpret_cast<float4*>(base + row * n_leaves),
+                       in[u] ? make_float4(slope[0], slope[1], slope[2], slope[3]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+            else
+                __stcs(base + row * n_leaves, in[u] ? slope[0] : 0.0f);
+        }
+    }
+}
+
+// ---- back to the node logits -----------------------------------------------------------------------
+
+// The balance loss's slope of every leaf, less their mean dloss / n: a slope that is the same for all leaves moves no logit, and
+// without it the differences between leaves are exact, (L counts_j - n) dloss / n^2.
+__device__ __forceinline__ float centred_slope(int32_t count, int n_leaves, double n, double dloss) {
+    return n > 0.0 ? (float)(dloss * ((double)n_leaves * (double)count - n) / (n * n)) : 0.0f;
+}
+
+__global__ void __launch_bounds__(1024)
+k_balance_slope(const int32_t* __restrict__ counts, const float* __restrict__ dloss, float* __restrict__ slope, int n_leaves)
+{
+    __shared__ double s_red[32];
+    pdl_trigger();
+    pdl_wait();
+    const double n = counted_tokens(counts, n_leaves, s_red), g = (double)__ldg(dloss);
+    for (int j = blockIdx.x * blockDim.x + threadIdx.x; j < n_leaves; j += gridDim.x * blockDim.x)
+        slope[j] = centred_slope(__ldg(counts + j), n_leaves, n, g);
+}
+
+constexpr int kRouteThreads = 256;
+constexpr int kRoutePerSm = 3;                // CTAs per SM
+constexpr int kRouteWarps = kRouteThreads / 32;
+constexpr int kRouteChunk = 128;              // leaves that one warp reduces at a time: four per lane, seven levels
+constexpr int kRouteStaged = 8192;            // floats of output staged in shared memory per step of a CTA
+constexpr int kRouteMaxStagedLeaves = 4096;   // ... beside the slopes of up to this many leaves
+
+// Rows that a CTA takes at a time: where they are staged a multiple of four, so that their outputs start on a 16-byte boundary.
+__host__ __device__ inline bool route_staged(int n_leaves) { return n_leaves <= kRouteMaxStagedLeaves; }
+__host__ __device__ inline int route_rows(int n_leaves) {
+    return !route_staged(n_leaves) ? 1 : n_leaves >= kRouteStaged / 4 ? 4 : kRouteStaged / n_leaves;
+}
+__host__ inline size_t route_smem(int n_leaves, bool balance) {
+    const size_t rows = route_rows(n_leaves), chunks = (size_t)n_leaves / kRouteChunk;
+    size_t floats = 2 * rows * (chunks > 1 ? chunks : 0);                                    // sums of the chunks
+    if (route_staged(n_leaves)) floats += rows * (n_leaves - 1) + 4 + (balance ? n_leaves : 0);
+    return floats * sizeof(float) + 16;
+}
+
+// One node: sums over its two children's leaves in, its own out.  Children too small for float32 have no say.
+__device__ __forceinline__ float node_gradient(float ml, float sl, float mr, float sr, float& m, float& s) {
+    m = ml + mr;
+    s = sl + sr;
+    const float inv = rcp_approx(m);
+    const float g = sr * (ml * inv) - sl * (mr * inv);
+    return m < FLT_MIN ? 0.0f : g;
+}
+
+// kUp: dmixture given; kBal: counts and dloss given (slope table for more than kRouteMaxStagedLeaves leaves).
+// A CTA takes route_rows rows at a time; its warps reduce chunks of 128 leaves (four levels in a lane's registers and across
+// neighbouring lanes, seven in all), then the levels above; the rows' gradients are collected in shared memory and leave as
+// aligned 16-byte vectors (a row has 2^d - 1 of them, so rows start anywhere).  Rows with a zero mask give zeros.
+template <bool kUp, bool kBal>
+__global__ void __launch_bounds__(kRouteThreads, kRoutePerSm)
+k_routing_backward(const float* __restrict__ mix, const float* __restrict__ dmix, const int32_t* __restrict__ leaf_idx,
+                   const uint8_t* __restrict__ mask, const int32_t* __restrict__ counts, const float* __restrict__ dloss,
+                   const float* __restrict__ slope_table, float* __restrict__ dz, int64_t B, int depth)
+{
+    extern __shared__ __align__(16) float s_route[];
+    __shared__ double s_red[kRouteWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int L = 1 << depth, N = L - 1;
+    const int R = route_rows(L), chunks = L >> 7;                        // chunks per row (0: several rows per chunk)
+    const bool staged = route_staged(L);
+    float* s_out = s_route;                                              // [R][N]
+    float* s_top = s_route + (staged ? ((R * N + 3) & ~3) : 0);          // [2][R][chunks]
+    float* s_slope = s_top + (chunks > 1 ? 2 * R * chunks : 0);          // [L]
+    pdl_trigger();
+    pdl_wait();
+    if (kBal && staged) {
+        const double n = counted_tokens(counts, L, s_red), g = (double)__ldg(dloss);
+        for (int j = tid; j < L; j += kRouteThreads) s_slope[j] = centred_slope(__ldg(counts + j), L, n, g);
+        __syncthreads();
+    }
+    const int64_t groups = (B + R - 1) / R;
+    for (int64_t grp = blockIdx.x; grp < groups; grp += gridDim.x) {
+        const int64_t row0 = grp * R;
+        const int rows = (int)min((int64_t)R, B - row0);
+        const int64_t elems = (int64_t)rows * L;
+        const int units = (int)((elems + kRouteChunk - 1) / kRouteChunk);
+        const float* gm = mix + row0 * L;
+        const float* gd = kUp ? dmix + row0 * L : nullptr;
+        float* out = staged ? s_out : dz + row0 * N;
+        constexpr int U = 4;                                             // chunks whose loads are in flight
+        for (int u0 = warp; u0 < units; u0 += U * kRouteWarps) {
+            float m4[U][4], g4[U][4];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int64_t e = (int64_t)(u0 + i * kRouteWarps) * kRouteChunk + lane * 4;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { m4[i][k] = 0.0f; g4[i][k] = 0.0f; }
+                if (e >= elems) continue;
+                if (depth >= 2 || e + 4 <= elems) {
+                    const float4 q = __ldcs(reinterpret_cast<const float4*>(gm + e));
+                    m4[i][0] = q.x; m4[i][1] = q.y; m4[i][2] = q.z; m4[i][3] = q.w;
+                    if constexpr (kUp) {
+                        const float4 d = __ldcs(reinterpret_cast<const float4*>(gd + e));
+                        g4[i][0] = d.x; g4[i][1] = d.y; g4[i][2] = d.z; g4[i][3] = d.w;
+                    }
+                } else {
+                    for (int k = 0; k < 2; ++k) {
+                        m4[i][k] = gm[e + k];
+                        if constexpr (kUp) g4[i][k] = gd[e + k];
+                    }
+                }
+                // the lane's row, or (L = 2) its two rows
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (half == 1 && (depth >= 2 || e + 2 >= elems)) break;
+                    const int64_t b = row0 + ((e + 2 * half) >> depth);
+                    const int k0 = 2 * half, k1 = depth >= 2 ? 4 : k0 + 2;
+                    if (kBal && (!leaf_idx || (unsigned)__ldg(leaf_idx + b) < (unsigned)L)) {
+                        const float* table = (staged ? s_slope : slope_table) + (depth >= 2 ? (int)(e & (L - 1)) : -k0);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (k >= k0 && k < k1) g4[i][k] += table[k];
+                    }
+                    if (mask && __ldg(mask + b) == 0) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (k >= k0 && k < k1) m4[i][k] = g4[i][k] = 0.0f;
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int unit = u0 + i * kRouteWarps;
+                if (unit >= units) break;
+                const int64_t e = (int64_t)unit * kRouteChunk + lane * 4;
+                const bool in = e < elems;
+                const int row = (int)(e >> depth), j = (int)(e & (L - 1));
+                float* o = out + (int64_t)row * N;
+                const float (&m)[4] = m4[i];
+                float ma, sa, mb, sb;
+                const float g0 = node_gradient(m[0], m[0] * g4[i][0], m[1], m[1] * g4[i][1], ma, sa);
+                const float g1 = node_gradient(m[2], m[2] * g4[i][2], m[3], m[3] * g4[i][3], mb, sb);
+                if (depth == 1) {
+                    if (in) {
+                        out[row] = g0;
+                        if (e + 2 < elems) out[row + 1] = g1;
+                    }
+                    continue;
+                }
+                const int last = (1 << (depth - 1)) - 1;                 // first node of the level above the leaves
+                if (in) {
+                    o[last + (j >> 1)] = g0;
+                    o[last + (j >> 1) + 1] = g1;
+                }
+                float mm, ss;
+                const float g2 = node_gradient(ma, sa, mb, sb, mm, ss);
+                if (in) o[(1 << (depth - 2)) - 1 + (j >> 2)] = g2;
+                // one more level per step: 2^k lanes share a node of level depth - 2 - k
+#pragma unroll
+                for (int k = 1; k <= 5; ++k) {
+                    if (k > depth - 2) break;
+                    const float mo = __shfl_xor_sync(kFullMask, mm, 1 << (k - 1)), so = __shfl_xor_sync(kFullMask, ss, 1 << (k - 1));
+                    const bool right = (lane >> (k - 1)) & 1;
+                    const float g = node_gradient(right ? mo : mm, right ? so : ss, right ? mm : mo, right ? ss : so, mm, ss);
+                    if (in && (lane & ((1 << k) - 1)) == 0) o[(1 << (depth - 2 - k)) - 1 + (j >> (2 + k))] = g;
+                }
+                if (chunks > 1 && lane == 0) {
+                    s_top[unit] = mm;                                    // unit = row * chunks + chunk
+                    s_top[R * chunks + unit] = ss;
+                }
+            }
+        }
+        if (chunks > 1) {
+            // the levels above the chunks: a warp per row, in place (a step's reads lie ahead of its writes)
+            __syncthreads();
+            for (int row = warp; row < rows; row += kRouteWarps) {
+                float* tm = s_top + row * chunks;
+                float* ts = tm + R * chunks;
+                float* o = out + (int64_t)row * N;
+                for (int nodes = chunks >> 1; nodes >= 1; nodes >>= 1) {
+                    for (int p0 = 0; p0 < nodes; p0 += 32) {
+                        const int p = p0 + lane;
+                        float mm = 0.0f, ss = 0.0f;
+                        if (p < nodes) o[nodes - 1 + p] = node_gradient(tm[2 * p], ts[2 * p], tm[2 * p + 1], ts[2 * p + 1], mm, ss);
+                        __syncwarp();
+                        if (p < nodes) { tm[p] = mm; ts[p] = ss; }
+                        __syncwarp();
+                    }
+                }
+            }
+        }
+        if (staged) {
+            __syncthreads();
+            float* dst = dz + row0 * N;
+            const int total = rows * N;
+            for (int i = tid; i < total >> 2; i += kRouteThreads) __stcs(reinterpret_cast<float4*>(dst) + i, reinterpret_cast<const float4*>(s_out)[i]);
+            for (int i = (total & ~3) + tid; i < total; i += kRouteThreads) dst[i] = s_out[i];
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace fff

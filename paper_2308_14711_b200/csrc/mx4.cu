@@ -1,0 +1,145 @@
+// Launchers of the microscaled 4-bit kernels (kernels/mx4.cuh); arguments are checked by their callers in fff_api.cu.
+#include "kernels/mx4.cuh"
+
+#include <algorithm>
+#include <mutex>
+
+#include "launch.h"
+
+namespace fff {
+
+namespace {
+
+constexpr int kMaxDevices = 64;
+std::mutex g_mu;
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Widest access to 16 consecutive elements at a multiple of 16 in rows of `cols` bf16 values: 32, 16 or 2 bytes.
+int access_bytes(const void* p, int cols) {
+    if (cols % 16 == 0 && aligned(p, 32)) return 32;
+    return cols % 8 == 0 && aligned(p, 16) ? 16 : 2;
+}
+
+MxLayout layout(const Mx4Layer& m) { return MxLayout{m.D, m.O, m.l, m.mma}; }
+
+// CTAs for `units` threads' work, at most `per_sm` per SM.
+unsigned spread(int64_t units, int threads, int sm_count, int per_sm) {
+    return (unsigned)std::max<int64_t>(1, std::min<int64_t>((units + threads - 1) / threads, (int64_t)sm_count * per_sm));
+}
+
+template <typename T>
+cudaError_t quantize(const LaunchOn& on, const T* src, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales, T* values) {
+    const unsigned grid = spread((rows * mx_scales(cols) * 4 + 1) / 2, 256, on.sm_count, 8);
+    return launch_on(on, cols % kMxBlock == 0 ? k_quantize_mx4<T, true> : k_quantize_mx4<T, false>, grid, 1, 256, 0, src, codes, scales, values,
+                     rows, cols);
+}
+
+template <typename T>
+cudaError_t dequantize(const LaunchOn& on, const uint8_t* codes, const uint8_t* scales, T* values, int64_t rows, int64_t cols) {
+    const unsigned grid = spread(rows * mx_scales(cols) * 4, 256, on.sm_count, 16);
+    return launch_on(on, cols % kMxBlock == 0 ? k_dequantize_mx4<T, true> : k_dequantize_mx4<T, false>, grid, 1, 256, 0, codes, scales, values,
+                     rows, cols);
+}
+
+template <int NT, bool kBig>
+cudaError_t launch_tiles(const LaunchOn& on, const MxLeafArgs& a, int n_tiles) {
+    const int smem = MxLeafSmem<NT>::bytes(a.tile_rows, a.lay.Kp(), a.counts ? a.n_leaves : 0);
+    static bool raised[kMaxDevices] = {};
+    {
+        std::lock_guard<std::mutex> lk(g_mu);
+        if (!raised[on.device]) {
+            const cudaError_t e = cudaFuncSetAttribute(k_leaf_mx4<NT, kBig>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+            if (e != cudaSuccess) return e;
+            raised[on.device] = true;
+        }
+    }
+    const int per_sm = std::max(1, std::min(2, 227 * 1024 / (smem + 1536)));
+    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)on.sm_count * per_sm, n_tiles));
+    return launch_on(on, k_leaf_mx4<NT, kBig>, grid, 1, kMxThreads, (size_t)smem, a);
+}
+
+}  // namespace
+
+cudaError_t quantize_mx4(const LaunchOn& on, const void* src, int elem_bytes, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales,
+                         void* values) {
+    return elem_bytes == 4 ? quantize(on, (const float*)src, rows, cols, codes, scales, (float*)values)
+                           : quantize(on, (const __nv_bfloat16*)src, rows, cols, codes, scales, (__nv_bfloat16*)values);
+}
+
+cudaError_t dequantize_mx4(const LaunchOn& on, const uint8_t* codes, const uint8_t* scales, int elem_bytes, int64_t rows, int64_t cols,
+                           void* values) {
+    return elem_bytes == 4 ? dequantize(on, codes, scales, (float*)values, rows, cols)
+                           : dequantize(on, codes, scales, (__nv_bfloat16*)values, rows, cols);
+}
+
+// (leaves of fewer than 8 neurons would leave most of an MMA's columns empty)
+bool mx4_on_tensor_cores(int leaf_width) { return leaf_width >= 8; }
+
+Mx4Bytes mx4_image_bytes(const Mx4Layer& m, int64_t n_leaves) {
+    const MxLayout L = layout(m);
+    return Mx4Bytes{(size_t)(L.w1() * n_leaves), (size_t)(L.s1() * n_leaves), (size_t)(L.w2() * n_leaves), (size_t)(L.s2() * n_leaves)};
+}
+
+cudaError_t mx4_find_big(const uint8_t* scales, int64_t n, int* flag, int sm_count) {
+    k_mx_find_big<<<spread(n, 256, sm_count, 8), 256>>>(scales, n, flag);
+    return cudaGetLastError();
+}
+
+cudaError_t mx4_pack(const Mx4Layer& m, const uint8_t* w1, const uint8_t* s1, const uint8_t* w2, const uint8_t* s2, int64_t n_leaves,
+                     int sm_count) {
+    k_pack_mx4<<<(unsigned)sm_count * 8, 256>>>(w1, s1, w2, s2, m.w1, m.s1, m.w2, m.s2, layout(m), n_leaves, m.big);
+    return cudaGetLastError();
+}
+
+cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* perm, const void* tiles, int n_tiles,
+                           int tile_rows, int32_t* counts, int n_leaves, int cap) {
+    MxLeafArgs a = {};
+    a.x = (const __nv_bfloat16*)t.x;
+    a.perm = perm;
+    a.tiles = (const Tile*)tiles;
+    a.n_tiles = n_tiles;
+    a.counts = counts;
+    a.n_leaves = n_leaves;
+    a.cap = cap;
+    a.w1 = m.w1; a.w2 = m.w2; a.s1 = m.s1; a.s2 = m.s2;
+    a.b1 = (const __nv_bfloat16*)t.b1;
+    a.b2 = (const __nv_bfloat16*)t.b2;
+    a.y = (__nv_bfloat16*)t.y;
+    a.lay = layout(m);
+    a.act = t.act;
+    a.tile_rows = tile_rows;
+    a.x_bytes = access_bytes(t.x, m.D);
+    a.y_bytes = access_bytes(t.y, m.O);
+    if (m.l <= 16) return m.big ? launch_tiles<2, true>(on, a, n_tiles) : launch_tiles<2, false>(on, a, n_tiles);
+    return m.big ? launch_tiles<4, true>(on, a, n_tiles) : launch_tiles<4, false>(on, a, n_tiles);
+}
+
+cudaError_t mx4_leaf_rows(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* leaf_idx, const int32_t* perm, int64_t B,
+                          const Mx4Tail& tail) {
+    MxRowsArgs a = {};
+    a.x = (const __nv_bfloat16*)t.x;
+    a.leaf_idx = leaf_idx;
+    a.perm = perm;
+    a.w1 = m.w1; a.w2 = m.w2; a.s1 = m.s1; a.s2 = m.s2;
+    a.b1 = (const __nv_bfloat16*)t.b1;
+    a.b2 = (const __nv_bfloat16*)t.b2;
+    a.y = (__nv_bfloat16*)t.y;
+    a.lay = layout(m);
+    a.act = t.act;
+    a.B = B;
+    a.x_vec = access_bytes(t.x, m.D) >= 16;
+    a.y_vec = access_bytes(t.y, m.O) >= 16;
+    a.big = m.big;
+    a.node_w = (const __nv_bfloat16*)tail.node_w;
+    a.node_b = (const __nv_bfloat16*)tail.node_b;
+    a.level0 = tail.level0;
+    a.levels = tail.levels;
+    a.pos = tail.pos;
+    a.leaf_out = tail.leaf_out;
+    const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((B + kMxRowWarps - 1) / kMxRowWarps, (int64_t)on.sm_count * 8));
+    return launch_on(on, tail.levels > 0 ? k_leaf_mx4_rows<true> : k_leaf_mx4_rows<false>, grid, 1, kMxRowWarps * 32,
+                     sizeof(float) * (size_t)kMxRowWarps * m.l, a);
+}
+
+}  // namespace fff
