@@ -294,7 +294,7 @@ void prof_free(fff_handle_s* h) {
 
 void release(fff_handle_s* h) {
     dfree(h->w2t);
-    dfree(h->mx.w1); dfree(h->mx.w2); dfree(h->mx.s1); dfree(h->mx.s2); dfree(h->bal_scratch);
+    dfree(h->mx.image); dfree(h->bal_scratch);
     dfree(h->node_w); dfree(h->node_b); dfree(h->w1); dfree(h->b1); dfree(h->w2); dfree(h->b2);
     dfree(h->ws_leaf); dfree(h->ws_perm); dfree(h->ws_perm2); dfree(h->ws_offsets); dfree(h->ws_offsets2[0]); dfree(h->ws_offsets2[1]);
     dfree(h->d_status); dfree(h->st_x); dfree(h->st_y); dfree(h->st_leaf);
@@ -381,10 +381,11 @@ int leaf_mma_slots(const fff_handle_s* h, int tile_rows) {
     }
 }
 
-// Rows of a tile of the 4-bit leaf kernel: 64 where leaves have them and enough tiles are left for two CTAs per SM (a leaf's weights are
-// expanded once per 32 rows and once per tile), as long as the hidden values of a tile fit beside another CTA's.
+// Rows of a tile of the 4-bit leaf kernel: the most that shared memory holds (a leaf's weights are expanded once per tile), 32 where that
+// would leave fewer than two rounds of tiles.
 int mx4_tile_rows(const fff_handle_s* h, int64_t B) {
-    return h->l <= 128 && B > 32 * h->n_leaves && expected_tiles(h, B, 64) >= 2.0 * h->sm_count ? 64 : 32;
+    const int most = fff::mx4_most_rows(h->mx, (int)std::min<int64_t>(h->n_leaves, kMaxListedLeaves));
+    return expected_tiles(h, B, most) >= 4.0 * h->sm_count ? most : 32;
 }
 
 LeafPlan leaf_plan(const fff_handle_s* h, int64_t B) {
@@ -1063,7 +1064,7 @@ fff::LaunchOn launch_on_handle(const fff_handle_s* h, cudaStream_t st) {
 fff_status_t run_leaf_mx4_rows(fff_handle_s* h, const void* x, const int32_t* leaf_idx, const int32_t* perm, void* y, int64_t B,
                                cudaStream_t st, const DescentTail& tail, int32_t* leaf_out) {
     const fff::Mx4Tail walk{h->node_w, h->node_b, tail.level0, tail.levels, tail.pos, leaf_out};
-    if (fff::mx4_leaf_rows(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->b1, h->b2, h->act}, leaf_idx, perm, B, walk) != cudaSuccess)
+    if (fff::mx4_leaf_rows(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->act, h->d_status}, leaf_idx, perm, B, walk) != cudaSuccess)
         return cudaGetLastError(), FFF_ERR_CUDA;
     return launched(h, st, tail.levels > 0 ? "descent_tail+leaf_ff_mx4_rows" : "grouped_leaf_ff_mx4_rows");
 }
@@ -1072,7 +1073,7 @@ fff_status_t run_leaf_mx4_rows(fff_handle_s* h, const void* x, const int32_t* le
 fff_status_t run_leaf_mx4(fff_handle_s* h, const void* x, const int32_t* perm, void* y, int64_t B, int tile_rows, cudaStream_t st) {
     // direct lists: perm is the table of lists, the tiles come from its counts
     int32_t* counts = h->slots_now && perm == h->ws_slots ? h->ws_cursor : nullptr;
-    if (fff::mx4_leaf_tiles(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->b1, h->b2, h->act}, perm, h->ws_tiles,
+    if (fff::mx4_leaf_tiles(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->act, h->d_status}, perm, h->ws_tiles,
                             tile_list_len(B, tile_rows, (int)h->n_leaves), tile_rows, counts, (int)h->n_leaves, (int)h->slot_cap) != cudaSuccess)
         return cudaGetLastError(), FFF_ERR_CUDA;
     return launched(h, st, "grouped_leaf_ff_mx4");
@@ -1869,7 +1870,7 @@ fff_status_t make_mx4_images(fff_handle_s* h, const uint8_t* w1, const uint8_t* 
     const int64_t nl = h->n_leaves, n1 = nl * h->l * ((h->D + 31) / 32), n2 = nl * h->l * ((h->O + 31) / 32);
     h->mx.D = h->D; h->mx.O = h->O; h->mx.l = h->l;
     h->mx.mma = fff::mx4_on_tensor_cores(h->l);
-    const fff::Mx4Bytes bytes = fff::mx4_image_bytes(h->mx, nl);
+    if (!fff::mx4_record_fits(h->mx)) return FFF_ERR_UNSUPPORTED;
     int* flag = nullptr;
     int big = 0;
     fff_status_t s = clone((void**)&flag, nullptr, sizeof(int));
@@ -1878,11 +1879,8 @@ fff_status_t make_mx4_images(fff_handle_s* h, const uint8_t* w1, const uint8_t* 
         s = (cudaGetLastError(), FFF_ERR_CUDA);
     dfree(flag);
     h->mx.big = big != 0;
-    if (s == FFF_OK) s = dmalloc((void**)&h->mx.w1, bytes.w1);
-    if (s == FFF_OK) s = dmalloc((void**)&h->mx.s1, bytes.s1);
-    if (s == FFF_OK) s = dmalloc((void**)&h->mx.w2, bytes.w2);
-    if (s == FFF_OK) s = dmalloc((void**)&h->mx.s2, bytes.s2);
-    if (s == FFF_OK && fff::mx4_pack(h->mx, w1, s1, w2, s2, nl, h->sm_count) != cudaSuccess) s = (cudaGetLastError(), FFF_ERR_CUDA);
+    if (s == FFF_OK) s = dmalloc((void**)&h->mx.image, fff::mx4_image_bytes(h->mx, nl));
+    if (s == FFF_OK && fff::mx4_pack(h->mx, w1, s1, w2, s2, h->b1, h->b2, nl, h->sm_count) != cudaSuccess) s = (cudaGetLastError(), FFF_ERR_CUDA);
     return s;
 }
 

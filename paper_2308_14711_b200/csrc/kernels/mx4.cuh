@@ -203,19 +203,27 @@ __device__ __forceinline__ uint32_t mx_pair(uint32_t lo, uint32_t hi) { return (
 
 constexpr int kMxUnit = 64;            // columns of x per step of the first product, outputs per step of the second
 
-// Sizes of the images of a layer.  Leaves of 8 neurons and more (tensor cores): the operands of mma.sync in the order in which a
-// warp loads them.  Thinner ones (CUDA cores): rows.  In both a row's columns are padded with zero codes.
+// A layer's image: one record per leaf with everything that its evaluation reads, so that one request brings it: codes of W1, their
+// scales, codes of W2, their scales, both biases (bf16).  Leaves of 8 neurons and more (tensor cores): the operands of mma.sync in the
+// order in which a warp loads them.  Thinner ones (CUDA cores): rows.  In both a row's columns are padded with zero codes.
 struct MxLayout {
     int D, O, l;
     bool mma;
     __host__ __device__ int units1() const { return (D + kMxUnit - 1) / kMxUnit; }
     __host__ __device__ int units2() const { return (O + kMxUnit - 1) / kMxUnit; }
     __host__ __device__ int Kp() const { return l <= 16 ? 16 : (l + 31) / 32 * 32; }      // hidden units as the second product sees them
-    // per leaf, in bytes
-    __host__ __device__ int64_t w1() const { return mma ? (int64_t)units1() * l * 32 : (int64_t)l * ((D + 7) / 8) * 4; }
-    __host__ __device__ int64_t s1() const { return mma ? (int64_t)units1() * l * 2 : (int64_t)l * mx_scales(D); }
-    __host__ __device__ int64_t w2() const { return mma ? (int64_t)units2() * Kp() * 32 : (int64_t)l * ((O + 7) / 8) * 4; }
-    __host__ __device__ int64_t s2() const { return mma ? (int64_t)units2() * 2 * Kp() : (int64_t)l * mx_scales(O); }
+    // sizes of the parts, then their places in the record, in bytes
+    __host__ __device__ int w1() const { return mma ? units1() * l * 32 : l * ((D + 7) / 8) * 4; }
+    __host__ __device__ int s1() const { return mma ? units1() * l * 2 : l * (int)mx_scales(D); }
+    __host__ __device__ int w2() const { return mma ? units2() * Kp() * 32 : l * ((O + 7) / 8) * 4; }
+    __host__ __device__ int s2() const { return mma ? units2() * 2 * Kp() : l * (int)mx_scales(O); }
+    __host__ __device__ static int up(int bytes) { return (bytes + 15) & ~15; }
+    __host__ __device__ int at_s1() const { return up(w1()); }
+    __host__ __device__ int at_w2() const { return at_s1() + up(s1()); }
+    __host__ __device__ int at_s2() const { return at_w2() + up(w2()); }
+    __host__ __device__ int at_b1() const { return at_s2() + up(s2()); }
+    __host__ __device__ int at_b2() const { return at_b1() + up(2 * l); }
+    __host__ __device__ int record() const { return (at_b2() + up(2 * O) + 127) & ~127; }
 };
 
 __device__ __forceinline__ uint32_t caller_code(const uint8_t* __restrict__ codes, int64_t row, int cols, int c) {
@@ -236,67 +244,62 @@ __global__ void k_mx_find_big(const uint8_t* __restrict__ scales, int64_t n, int
 
 // w1: caller's codes [leaves * l, D]; w2: [leaves * l, O].
 __global__ void k_pack_mx4(const uint8_t* __restrict__ w1, const uint8_t* __restrict__ sc1, const uint8_t* __restrict__ w2,
-                           const uint8_t* __restrict__ sc2, uint32_t* __restrict__ w1img, uint8_t* __restrict__ s1img,
-                           uint32_t* __restrict__ w2img, uint8_t* __restrict__ s2img, MxLayout L, int64_t n_leaves, bool big)
+                           const uint8_t* __restrict__ sc2, const uint16_t* __restrict__ b1, const uint16_t* __restrict__ b2,
+                           unsigned char* __restrict__ img, MxLayout L, int64_t n_leaves, bool big)
 {
     const int64_t i0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, step = (int64_t)gridDim.x * blockDim.x;
-    const int l = L.l, D = L.D, O = L.O;
+    const int l = L.l, D = L.D, O = L.O, Kp = L.Kp();
+    const int64_t record = L.record();
     auto word_of = [&](const uint8_t* codes, int64_t row, int cols, int c0) {
         uint32_t c[8];
         for (int e = 0; e < 8; ++e) c[e] = caller_code(codes, row, cols, c0 + e);
         return mx_image_word(c);
     };
+    // n words (or bytes) per leaf from offset `at` on: k of leaf j is value(j, k)
+    auto words = [&](int at, int n, auto&& value) {
+        for (int64_t i = i0; i < n_leaves * n; i += step) {
+            const int64_t leaf = i / n;
+            reinterpret_cast<uint32_t*>(img + leaf * record + at)[i - leaf * n] = value(leaf, (int)(i - leaf * n));
+        }
+    };
+    auto bytes = [&](int at, int n, auto&& value) {
+        for (int64_t i = i0; i < n_leaves * n; i += step) {
+            const int64_t leaf = i / n;
+            (img + leaf * record + at)[i - leaf * n] = value(leaf, (int)(i - leaf * n));
+        }
+    };
+    for (int64_t i = i0; i < n_leaves * l; i += step) reinterpret_cast<uint16_t*>(img + i / l * record + L.at_b1())[i % l] = b1[i];
+    for (int64_t i = i0; i < n_leaves * O; i += step) reinterpret_cast<uint16_t*>(img + i / O * record + L.at_b2())[i % O] = b2[i];
     if (!L.mma) {
-        const int wd = (D + 7) / 8, wo = (O + 7) / 8;
-        for (int64_t i = i0; i < n_leaves * l * wd; i += step) w1img[i] = word_of(w1, i / wd, D, (int)(i % wd) * 8);
-        for (int64_t i = i0; i < n_leaves * l * wo; i += step) w2img[i] = word_of(w2, i / wo, O, (int)(i % wo) * 8);
-        const int nd = (int)mx_scales(D), no = (int)mx_scales(O);
-        for (int64_t i = i0; i < n_leaves * l * nd; i += step) s1img[i] = image_scale(sc1, i / nd, D, (int)(i % nd) * kMxBlock, big);
-        for (int64_t i = i0; i < n_leaves * l * no; i += step) s2img[i] = image_scale(sc2, i / no, O, (int)(i % no) * kMxBlock, big);
+        const int wd = (D + 7) / 8, wo = (O + 7) / 8, nd = (int)mx_scales(D), no = (int)mx_scales(O);
+        words(0, l * wd, [&](int64_t leaf, int k) { return word_of(w1, leaf * l + k / wd, D, k % wd * 8); });
+        words(L.at_w2(), l * wo, [&](int64_t leaf, int k) { return word_of(w2, leaf * l + k / wo, O, k % wo * 8); });
+        bytes(L.at_s1(), l * nd, [&](int64_t leaf, int k) { return image_scale(sc1, leaf * l + k / nd, D, k % nd * kMxBlock, big); });
+        bytes(L.at_s2(), l * no, [&](int64_t leaf, int k) { return image_scale(sc2, leaf * l + k / no, O, k % no * kMxBlock, big); });
         return;
     }
-    // W1: [leaf][unit][row][quarter of the unit's 64 columns][2 words]
-    const int64_t n1 = L.w1() / 4, n2 = L.w2() / 4;
-    for (int64_t i = i0; i < n_leaves * n1; i += step) {
-        const int64_t leaf = i / n1, k = i - leaf * n1;
-        const int u = (int)(k / (l * 8)), row = (int)(k % (l * 8)) / 8, q = (int)(k & 7);
-        w1img[i] = word_of(w1, leaf * l + row, D, u * kMxUnit + q * 8);
-    }
-    for (int64_t i = i0; i < n_leaves * L.s1(); i += step) {
-        const int64_t leaf = i / L.s1(), k = i - leaf * L.s1();
-        const int u = (int)(k / (l * 2)), row = (int)(k % (l * 2)) / 2, b = (int)(k & 1);
-        s1img[i] = image_scale(sc1, leaf * l + row, D, u * kMxUnit + b * kMxBlock, big);
-    }
-    // W2: [leaf][unit of 64 outputs][block of 32 hidden units][half of the 8 output tiles][lane][4 words], a word: the 8 hidden units
-    // 8c.. of one output; with 16 hidden units [leaf][unit][lane][4 words], a word: the 4 units 4c.. of two outputs.  Output of tile i
-    // and lane (g, c): 16 (g / 2) + 2 i + g % 2.
-    const int Kp = L.Kp();
-    for (int64_t i = i0; i < n_leaves * n2; i += step) {
-        const int64_t leaf = i / n2, k = i - leaf * n2;
-        const int u = (int)(k / (Kp * 8)), in = (int)(k % (Kp * 8));
-        const int j = in & 3, lane = (in >> 2) & 31, g = lane >> 2, c = lane & 3;
+    // W1: [unit of 64 columns][row][quarter of the unit][2 words]; scales [unit][row][half of the unit]
+    words(0, L.w1() / 4, [&](int64_t leaf, int k) { return word_of(w1, leaf * l + k % (l * 8) / 8, D, k / (l * 8) * kMxUnit + (k & 7) * 8); });
+    bytes(L.at_s1(), L.s1(), [&](int64_t leaf, int k) {
+        return image_scale(sc1, leaf * l + k % (l * 2) / 2, D, k / (l * 2) * kMxUnit + (k & 1) * kMxBlock, big);
+    });
+    // W2: [unit of 64 outputs][block of 32 hidden units][half of the 8 words][lane][4 words], word 2i + r: the hidden units 8c.. of output
+    // 8g + 2i + r, lane = (g, c); with 16 hidden units [unit][lane][4 words], word i: units 4c.. of outputs 8g + 2i, then of 8g + 2i + 1.
+    words(L.at_w2(), L.w2() / 4, [&](int64_t leaf, int k) {
+        const int u = k / (Kp * 8), in = k % (Kp * 8), j = in & 3, lane = (in >> 2) & 31, g = lane >> 2, c = lane & 3;
         uint32_t code[8];
         for (int e = 0; e < 8; ++e) {
-            int tile, unit;
-            if (Kp == 16) {
-                tile = 2 * j + (e >> 2);
-                unit = 4 * c + (e & 3);
-            } else {
-                const int kb = in >> 8, half = (in >> 7) & 1;
-                tile = half * 4 + j;
-                unit = kb * 32 + 8 * c + e;
-            }
-            const int o = u * kMxUnit + 16 * (g >> 1) + 2 * tile + (g & 1);
-            code[e] = unit < l ? caller_code(w2, leaf * l + unit, O, o) : 0u;
+            const int word = Kp == 16 ? 2 * j + (e >> 2) : ((in >> 7) & 1) * 4 + j;
+            const int unit = Kp == 16 ? 4 * c + (e & 3) : (in >> 8) * 32 + 8 * c + e;
+            code[e] = unit < l ? caller_code(w2, leaf * l + unit, O, u * kMxUnit + 8 * g + word) : 0u;
         }
-        w2img[i] = mx_image_word(code);
-    }
-    // [leaf][unit][half of its outputs][hidden unit]
-    for (int64_t i = i0; i < n_leaves * L.s2(); i += step) {
-        const int64_t leaf = i / L.s2(), k = i - leaf * L.s2();
-        const int u = (int)(k / (2 * Kp)), b = (int)(k / Kp) & 1, unit = (int)(k % Kp);
-        s2img[i] = unit < l ? image_scale(sc2, leaf * l + unit, O, u * kMxUnit + b * kMxBlock, big) : (uint8_t)(big ? 0 : 126);
-    }
+        return mx_image_word(code);
+    });
+    // scales [unit][half of its outputs][hidden unit]
+    bytes(L.at_s2(), L.s2(), [&](int64_t leaf, int k) {
+        const int u = k / (2 * Kp), unit = k % Kp;
+        return unit < l ? image_scale(sc2, leaf * l + unit, O, u * kMxUnit + k / Kp % 2 * kMxBlock, big) : (uint8_t)(big ? 0 : 126);
+    });
 }
 
 // ---- leaves on tensor cores ------------------------------------------------------------------------
@@ -308,293 +311,435 @@ struct MxLeafArgs {
     int n_tiles;
     int32_t* counts;                   // entries of every list, [1] CTAs that have finished; zeroed at the end
     int n_leaves, cap;
-    const uint32_t *w1, *w2;
-    const uint8_t *s1, *s2;
-    const __nv_bfloat16 *b1, *b2;      // caller layout
+    const unsigned char* image;        // records of the leaves
     __nv_bfloat16* y;
     MxLayout lay;
-    int act, tile_rows;                // tile_rows: 32 or 64
-    int x_bytes, y_bytes;              // widest access that rows of x / y allow: 32, 16 or 2
+    int act, tile_rows;                // tile_rows: a multiple of 8, at most 8 kMxMaxGroups
+    int x_bytes, y_bytes;              // widest access that rows of x and y allow, 16 or 2
+    int* status;
 };
 
-constexpr int kMxWarps = 8;
-constexpr int kMxThreads = kMxWarps * 32;
-
-// 16 consecutive columns of a row (columns past n read as zero).
-__device__ __forceinline__ void mx_load16(const __nv_bfloat16* __restrict__ p, int n, int width, uint32_t (&r)[8]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = 0u;
-    if (width == 32) {
-        if (n > 0)
-            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p));
-    } else if (width == 16) {
-        if (n > 0) { const uint4 a = __ldg(reinterpret_cast<const uint4*>(p)); r[0] = a.x; r[1] = a.y; r[2] = a.z; r[3] = a.w; }
-        if (n > 8) { const uint4 a = __ldg(reinterpret_cast<const uint4*>(p) + 1); r[4] = a.x; r[5] = a.y; r[6] = a.z; r[7] = a.w; }
-    } else {
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (2 * i < n) r[i] = __ldg(q + 2 * i);
-            if (2 * i + 1 < n) r[i] |= (uint32_t)__ldg(q + 2 * i + 1) << 16;
-        }
-    }
-}
-__device__ __forceinline__ void mx_store16(__nv_bfloat16* __restrict__ p, int n, int width, const uint32_t (&r)[8]) {
-    if (width == 32) {
-        if (n > 0) ptx::st_global_v8(p, r);
-    } else if (width == 16) {
+// 8 consecutive outputs.
+__device__ __forceinline__ void mx_store8(__nv_bfloat16* __restrict__ p, int n, bool vec, const uint32_t (&r)[4]) {
+    if (vec) {
         if (n > 0) __stcs(reinterpret_cast<uint4*>(p), make_uint4(r[0], r[1], r[2], r[3]));
-        if (n > 8) __stcs(reinterpret_cast<uint4*>(p) + 1, make_uint4(r[4], r[5], r[6], r[7]));
     } else {
         uint16_t* q = reinterpret_cast<uint16_t*>(p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
             if (2 * i < n) q[2 * i] = (uint16_t)r[i];
             if (2 * i + 1 < n) q[2 * i + 1] = (uint16_t)(r[i] >> 16);
         }
     }
 }
+// Sends for [p, p + bytes) into L2 (16-byte aligned, whole 16-byte units).
+__device__ __forceinline__ void mx_prefetch(const void* p, int64_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"((uint32_t)bytes) : "memory");
+}
 
-// Shared memory of k_leaf_mx4: partial sums of the first product, hidden values (two bf16 planes), the tile's tokens, and the number
-// of tiles before every leaf where tiles come from lists.
-template <int NT>
+constexpr int kMxWarps = 8;
+constexpr int kMxThreads = kMxWarps * 32;
+constexpr int kMxMaxGroups = 8;              // groups of 8 tokens per tile, at most
+constexpr int kMxChunk = 1024;               // columns of x in shared memory at a time, at most
+
+// Shared memory of k_leaf_mx4: token rows (at a pitch of 16 bytes past whole 128-byte lines: the operand loads of 8 rows then touch
+// every bank once), partial sums of the first product, hidden values (two bf16 planes), the tokens of this tile and the next, and the
+// number of tiles before every leaf and the rows of its last one where tiles come from lists.
 struct MxLeafSmem {
-    static constexpr int kRed = kMxWarps * 2 * NT * 4 * 32 * 4;
-    __host__ __device__ static int hidden(int tile_rows, int Kp) { return tile_rows * Kp * 4; }
-    __host__ __device__ static int bytes(int tile_rows, int Kp, int listed) {
-        return kRed + hidden(tile_rows, Kp) + tile_rows * 4 + (listed ? (listed + 1) * 2 + 2 : 0);
-    }
+    int rows, D, Kp, listed;
+    __host__ __device__ int chunk() const { return D < kMxChunk ? (D + kMxUnit - 1) / kMxUnit * kMxUnit : kMxChunk; }
+    __host__ __device__ int pitch() const { return chunk() * 2 + 16; }
+    __host__ __device__ int x() const { return rows * pitch(); }
+    __host__ __device__ int red() const { return kMxWarps * (rows / 8) * 512; }
+    __host__ __device__ int hid() const { return rows * Kp * 4; }
+    __host__ __device__ int bytes() const { return x() + red() + hid() + 2 * rows * 4 + (listed ? (listed + 1) * 2 + listed + 2 : 0); }
 };
 
-// Hidden layer of 32 rows and 8 NT units: this warp's share of the columns.  Token rows and codes go from global memory straight
-// into the operands of the MMAs: the order of the summands is free, so lane c of a quad takes 16 consecutive columns of its row (32
-// bytes of x, 8 of codes, one scale) for four MMAs.
-template <int NT, bool kBig>
-__device__ __forceinline__ void mx_hidden(const MxLeafArgs& A, const uint32_t* __restrict__ w1, const uint8_t* __restrict__ s1, const int (&tok)[4],
-                                          int unit0, int warp, int lane, float (&acc)[2][NT][4])
+// The operand registers of one word of W1 (16 columns: two words), scaled.
+template <bool kBig>
+__device__ __forceinline__ void mx_row16(uint2 code, uint32_t sc, uint32_t (&r)[8]) {
+    uint32_t lo[4], hi[4];
+    mx_expand(code.x, lo);
+    mx_expand(code.y, hi);
+    const uint32_t f1 = mx_mul1(sc, kBig), f2 = kBig ? mx_mul2(sc) : 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[i] = mul_bf16x2(lo[i], f1);
+        r[4 + i] = mul_bf16x2(hi[i], f1);
+        if (kBig) { r[i] = mul_bf16x2(r[i], f2); r[4 + i] = mul_bf16x2(r[4 + i], f2); }
+    }
+}
+
+// A warp's share of the first product for 16 hidden units and all tokens of the tile, over the columns in shared memory.  Weights are
+// the MMAs' 16 rows, tokens their 8 columns.  The order of the summands is free, so lane c of a quad takes 16 consecutive columns (32
+// bytes of a token's row, 8 of codes, one scale) for four MMAs.  Codes go from global memory straight into the operands, kMxAhead steps
+// ahead (all of a warp's steps for up to 1024 columns), the first of them sent for before the tokens are waited for.
+constexpr int kMxAhead = 4;
+struct MxCodes {
+    uint2 code[kMxAhead][2];
+    uint32_t sc[kMxAhead][2];
+};
+__device__ __forceinline__ void mx_fetch_codes(const unsigned char* __restrict__ rec, int at_s1, int l, int row0, int u, int u1, int lane, MxCodes& q, int k) {
+    const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int row = row0 + 8 * h + g;
+        const bool in = row < l && u < u1;
+        q.code[k][h] = in ? __ldg(reinterpret_cast<const uint2*>(rec) + (u * l + row) * 4 + c) : make_uint2(0u, 0u);
+        q.sc[k][h] = in ? __ldg(rec + at_s1 + (u * l + row) * 2 + (c >> 1)) : 0u;
+    }
+}
+template <bool kBig>
+__device__ __forceinline__ void mx_hidden(const unsigned char* __restrict__ rec, int at_s1, int l, MxCodes& q, const unsigned char* xs, int pitch,
+                                          int groups, int row0, int u0, int u1, int step, int unit_base, int lane, float (&acc)[kMxMaxGroups][4])
 {
-    const int g = lane >> 2, c = lane & 3, l = A.lay.l, D = A.lay.D;
+    const int g = lane >> 2, c = lane & 3;
+    for (int u = u0; u < u1; u += kMxAhead * step) {
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+        for (int k = 0; k < kMxAhead; ++k) {
+            const int uk = u + k * step;
+            if (uk >= u1) break;
+            uint32_t w[2][8];
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
+            for (int h = 0; h < 2; ++h) mx_row16<kBig>(q.code[k][h], q.sc[k][h], w[h]);
+            if (uk + kMxAhead * step < u1) mx_fetch_codes(rec, at_s1, l, row0, uk + kMxAhead * step, u1, lane, q, k);
+            const unsigned char* xp = xs + g * pitch + (uk - unit_base) * (kMxUnit * 2) + 32 * c;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
-    const bool two = __any_sync(kFullMask, tok[2] >= 0);
-    for (int u = warp; u < A.lay.units1(); u += kMxWarps) {
-        const int col = u * kMxUnit + 16 * c;
-        uint32_t xr[4][8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx_load16(A.x + (int64_t)max(tok[i], 0) * D + col, tok[i] >= 0 ? D - col : 0, A.x_bytes, xr[i]);
-        uint2 code[NT];
-        uint32_t sc[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const int row = unit0 + 8 * j + g;
-            const bool in = row < l;
-            code[j] = in ? __ldg(reinterpret_cast<const uint2*>(w1) + ((int64_t)u * l + row) * 4 + c) : make_uint2(0u, 0u);
-            sc[j] = in ? __ldg(s1 + ((int64_t)u * l + row) * 2 + (c >> 1)) : 0u;
-        }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            const uint32_t f1 = mx_mul1(sc[j], kBig), f2 = kBig ? mx_mul2(sc[j]) : 0u;
-            uint32_t b[8];
-            {
-                uint32_t lo[4], hi[4];
-                mx_expand(code[j].x, lo);
-                mx_expand(code[j].y, hi);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    b[i] = mul_bf16x2(lo[i], f1);
-                    b[4 + i] = mul_bf16x2(hi[i], f1);
-                    if (kBig) { b[i] = mul_bf16x2(b[i], f2); b[4 + i] = mul_bf16x2(b[4 + i], f2); }
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                ptx::mma_bf16(acc[0][j], xr[0][2 * s], xr[1][2 * s], xr[0][2 * s + 1], xr[1][2 * s + 1], b[2 * s], b[2 * s + 1]);
-                if (two) ptx::mma_bf16(acc[1][j], xr[2][2 * s], xr[3][2 * s], xr[2][2 * s + 1], xr[3][2 * s + 1], b[2 * s], b[2 * s + 1]);
+            for (int t = 0; t < kMxMaxGroups; ++t) {
+                if (t >= groups) break;
+                const uint4 a = *reinterpret_cast<const uint4*>(xp + t * 8 * pitch), b = *reinterpret_cast<const uint4*>(xp + t * 8 * pitch + 16);
+                ptx::mma_bf16(acc[t], w[0][0], w[1][0], w[0][1], w[1][1], a.x, a.y);
+                ptx::mma_bf16(acc[t], w[0][2], w[1][2], w[0][3], w[1][3], a.z, a.w);
+                ptx::mma_bf16(acc[t], w[0][4], w[1][4], w[0][5], w[1][5], b.x, b.y);
+                ptx::mma_bf16(acc[t], w[0][6], w[1][6], w[0][7], w[1][7], b.z, b.w);
             }
         }
     }
 }
 
-// One K-block of the second product: the eight output tiles' operands from their words.  K16: 16 hidden units (two words' worth of
-// tiles per word), else 32.
-template <bool K16, bool kBig>
-__device__ __forceinline__ void mx_output_operands(const uint4 (&word)[2], uint2 sc, uint32_t (&b)[8][K16 ? 2 : 4])
-{
-    // multipliers of the pairs of hidden units (the scales of a pair are neighbouring bytes)
-    constexpr int P = K16 ? 2 : 4;
-    uint32_t f1[P], f2[P];
-#pragma unroll
-    for (int p = 0; p < P; ++p) {
-        const uint32_t two = p < 2 ? sc.x : sc.y, lo = (two >> (16 * (p & 1))) & 0xffu, hi = (two >> (16 * (p & 1) + 8)) & 0xffu;
-        f1[p] = mx_pair(mx_mul1(lo, kBig), mx_mul1(hi, kBig));
-        f2[p] = kBig ? mx_pair(mx_mul2(lo), mx_mul2(hi)) : 0u;
+// The bin that tile idx belongs to: the last b with pre[b] <= idx.  By a whole warp: 32 places at a time.
+__device__ __forceinline__ int mx_bin_of_tile(const uint16_t* pre, int n_bins, int idx, int lane) {
+    int lo = 0, n = n_bins;                                // in [lo, lo + n)
+    while (n > 1) {
+        const int step = (n + 31) / 32, at = lo + lane * step;
+        const unsigned at_or_before = __ballot_sync(kFullMask, lane * step < n && pre[at] <= idx);
+        const int k = 31 - __clz(at_or_before);            // (pre is sorted and pre[lo] <= idx)
+        n = min(step, n - k * step);
+        lo += k * step;
     }
-    const uint32_t w[8] = {word[0].x, word[0].y, word[0].z, word[0].w, word[1].x, word[1].y, word[1].z, word[1].w};
-#pragma unroll
-    for (int i = 0; i < (K16 ? 4 : 8); ++i) {
-        uint32_t r[4];
-        mx_expand(w[i], r);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int tile = K16 ? 2 * i + (q >> 1) : i, p = K16 ? (q & 1) : q;
-            uint32_t v = mul_bf16x2(r[q], f1[p]);
-            if (kBig) v = mul_bf16x2(v, f2[p]);
-            b[tile][p] = v;
-        }
-    }
+    return lo;
 }
 
-// A CTA per tile of up to tile_rows tokens of one leaf.  The first product is split along D over the warps (no weight is expanded
-// twice), their sums meet in shared memory, where bias and activation are applied; for the second product every warp has output
-// columns of its own, numbered so that a lane ends with 16 consecutive outputs of its tokens.  Hidden values are kept as sums of two
-// bf16 values (float32 precision to 2^-18): the extra MMAs cost little next to the expansion.
-// NT: groups of 8 hidden units at a time: 2 for leaves of up to 16 (one K-block of 16 in the second product), else 4.
-template <int NT, bool kBig>
+// A CTA per tile of up to tile_rows tokens of one leaf, two CTAs per SM.  Token rows come by bulk copies; those of the next tile are
+// sent for as soon as this tile's first product is done with the buffer, and arrive while its hidden values and outputs are computed;
+// the next leaf's record is sent for to L2 at the same time.  The first product is split along D over the warps (MT = 2: over the two
+// groups of 16 hidden units too), so that no weight is expanded twice; the sums meet in shared memory, where bias and activation are
+// applied; for the second product every warp has output columns of its own, numbered so that a lane ends with 8 consecutive outputs
+// of its tokens and 8 lanes with 128 bytes of a row.  Hidden values are kept as sums of two bf16 values (float32 precision to 2^-16):
+// the extra MMAs cost little next to the expansion.
+// MT: groups of 16 hidden units at a time: 1 for leaves of up to 16 (one K-block of 16 in the second product), else 2.
+// kWide: more than 32 hidden units: several passes over x, several K-blocks in the second product.
+template <int MT, bool kWide, bool kBig>
 __global__ void __launch_bounds__(kMxThreads, 2)
 k_leaf_mx4(const MxLeafArgs A)
 {
-    using S = MxLeafSmem<NT>;
-    constexpr bool K16 = NT == 2;
+    static_assert(!kWide || MT == 2, "leaves of up to 16 have one K-block");
+    constexpr bool K16 = MT == 1;
+    constexpr int NW = kMxWarps, kThreads = kMxThreads, P = K16 ? 2 : 4;
+    constexpr int kSplit = NW / MT;                        // warps that share a group of 16 hidden units
     extern __shared__ __align__(16) unsigned char smem_mx[];
-    __shared__ int s_wsum[kMxWarps];
+    __shared__ int s_wsum[NW], s_last, s_next[3];          // s_next: tile, leaf, rows
+    __shared__ uint64_t s_full;
     const MxLayout& Ly = A.lay;
-    const int Kp = Ly.Kp(), l = Ly.l, O = Ly.O;
-    float* red = reinterpret_cast<float*>(smem_mx);                                   // [warp][m-tile, group, register][lane]
-    __nv_bfloat16* hid = reinterpret_cast<__nv_bfloat16*>(smem_mx + S::kRed);         // [2][tile_rows][Kp]
-    int* s_tok = reinterpret_cast<int*>(smem_mx + S::kRed + S::hidden(A.tile_rows, Kp));
-    uint16_t* s_pre = reinterpret_cast<uint16_t*>(s_tok + A.tile_rows);
-    const int plane = A.tile_rows * Kp;
+    const int l = Ly.l, D = Ly.D, O = Ly.O, Kp = K16 ? 16 : kWide ? Ly.Kp() : 32;
+    const int R = A.tile_rows;
+    const MxLeafSmem S{R, D, Kp, A.counts ? A.n_leaves : 0};
+    unsigned char* xs = smem_mx;
+    float* red = reinterpret_cast<float*>(smem_mx + S.x());                           // [warp][token group][register][lane]
+    __nv_bfloat16* hid = reinterpret_cast<__nv_bfloat16*>(smem_mx + S.x() + S.red()); // [2][R][Kp]
+    int* s_tok2 = reinterpret_cast<int*>(smem_mx + S.x() + S.red() + S.hid());        // [2][R]
+    uint16_t* s_pre = reinterpret_cast<uint16_t*>(s_tok2 + 2 * R);                    // [n_leaves + 1]
+    uint8_t* s_rest = reinterpret_cast<uint8_t*>(s_pre + A.n_leaves + 1);             // [n_leaves]
+    const int pitch = S.pitch(), chunk = S.chunk(), chunks = (D + chunk - 1) / chunk;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    if (tid == 0) {
+        ptx::mbar_init(&s_full, 1);
+        ptx::fence_mbar_init();
+    }
+    // columns past D stay zero: the copies do not touch them
+    for (int i = tid; i < S.x() / 16; i += kThreads) reinterpret_cast<uint4*>(xs)[i] = make_uint4(0u, 0u, 0u, 0u);
+    ptx::fence_proxy_async();
     pdl_trigger();
+    __syncthreads();
     pdl_wait();
-    if (A.counts) tiles_before_bins([&](int b) { return __ldcg(A.counts + b); }, A.n_leaves, A.tile_rows, s_pre, s_wsum, kMxThreads);
+    if (A.counts)
+        tiles_before_bins([&](int b) {
+            const int n = __ldcg(A.counts + b);
+            s_rest[b] = (uint8_t)((n + R - 1) % R + 1);
+            return n;
+        }, A.n_leaves, R, s_pre, s_wsum, kThreads);
     const int n_tiles = A.counts ? s_pre[A.n_leaves] : A.n_tiles;
-    const int units2 = Ly.units2(), kblocks = K16 ? 1 : Kp / 32;
+    const int units1 = Ly.units1(), units2 = Ly.units2(), kblocks = kWide ? Kp / 32 : 1;
+    const int64_t record = Ly.record();
+    const int at_s1 = Ly.at_s1(), at_w2 = Ly.at_w2(), at_s2 = Ly.at_s2(), at_b1 = Ly.at_b1(), at_b2 = Ly.at_b2();
+    const bool bulk = A.x_bytes >= 16;
 
-    for (int tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
-        int leaf, rows;
-        const int32_t* list;
+    // The first tile from `tile` on that is not empty (a list of tiles may contain empty ones); rows = 0: none.  Tokens `lane` and
+    // `lane + 32` of it in tok.  By a whole warp.
+    struct Found { int tile, leaf, rows, tok[2]; };
+    auto find_tile = [&](int tile) {
+        Found f;
+        f.tile = n_tiles;
+        f.leaf = f.rows = 0;
+        f.tok[0] = f.tok[1] = -1;
+        const int32_t* list = nullptr;
         if (A.counts) {
-            leaf = bin_of_tile(s_pre, A.n_leaves, tile);
-            const int first = (tile - s_pre[leaf]) * A.tile_rows;
-            rows = min(A.tile_rows, __ldcg(A.counts + leaf) - first);
-            list = A.perm + (int64_t)leaf * A.cap + first;
+            if (tile < n_tiles) {
+                f.tile = tile;
+                f.leaf = mx_bin_of_tile(s_pre, A.n_leaves, tile, lane);
+                f.rows = tile + 1 < s_pre[f.leaf + 1] ? R : s_rest[f.leaf];
+                list = A.perm + (int64_t)f.leaf * A.cap + (tile - s_pre[f.leaf]) * R;
+            }
         } else {
-            const Tile t = A.tiles[tile];
-            leaf = t.bin;
-            rows = t.rows;
-            list = A.perm + t.start;
+            for (; tile < n_tiles; tile += 32 * gridDim.x) {
+                const int64_t mine = tile + (int64_t)lane * gridDim.x;
+                Tile t;
+                t.rows = 0;
+                if (mine < n_tiles) t = A.tiles[mine];
+                const unsigned some = __ballot_sync(kFullMask, t.rows > 0);
+                if (some) {
+                    const int k = __ffs(some) - 1;
+                    f.tile = tile + k * gridDim.x;
+                    f.leaf = __shfl_sync(kFullMask, t.bin, k);
+                    f.rows = __shfl_sync(kFullMask, t.rows, k);
+                    list = A.perm + __shfl_sync(kFullMask, t.start, k);
+                    break;
+                }
+            }
         }
-        if (rows == 0) continue;                           // (a list of tiles may contain empty ones)
-        if (tid < A.tile_rows) s_tok[tid] = tid < rows ? __ldcg(list + tid) : -1;
-        const uint32_t* w1 = A.w1 + (int64_t)leaf * (Ly.w1() / 4);
-        const uint32_t* w2 = A.w2 + (int64_t)leaf * (Ly.w2() / 4);
-        const uint8_t* s1 = A.s1 + (int64_t)leaf * Ly.s1();
-        const uint8_t* s2 = A.s2 + (int64_t)leaf * Ly.s2();
-        // needed after the whole of the first product
-        for (int64_t off = (int64_t)tid * 128; off < Ly.w2(); off += kMxThreads * 128)
-            asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const unsigned char*>(w2) + off));
-        __syncthreads();
+        if (lane < f.rows) f.tok[0] = __ldcg(list + lane);
+        if (lane + 32 < f.rows) f.tok[1] = __ldcg(list + lane + 32);
+        return f;
+    };
+    // sends for columns [k0, k0 + chunk) of a tile's rows
+    auto send_x = [&](const Found& f, int k0) {
+        const int bytes = min(chunk, D - k0) * 2;
+        if (lane == 0) ptx::mbar_arrive_expect_tx(&s_full, (uint32_t)(bytes * f.rows));
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (f.tok[h] >= 0) ptx::bulk_g2s(xs + (lane + 32 * h) * pitch, A.x + (int64_t)f.tok[h] * D + k0, (uint32_t)bytes, &s_full);
+    };
+    auto announce = [&](const Found& f, int buf) {
+        if (lane < R) s_tok2[buf * R + lane] = f.tok[0];
+        if (lane + 32 < R) s_tok2[buf * R + lane + 32] = f.tok[1];
+        if (f.rows > 0) {
+            if (bulk) send_x(f, 0);
+            if (lane == 0) mx_prefetch(A.image + f.leaf * record, record);
+        }
+    };
+    Found mine, following;                                 // (warp 0)
+    if (warp == 0) {
+        mine = find_tile(blockIdx.x);
+        announce(mine, 0);
+        if (lane == 0) { s_next[0] = mine.tile; s_next[1] = mine.leaf; s_next[2] = mine.rows; }
+    }
+    __syncthreads();
+    uint32_t phase = 0;
+    bool timed_out = false;
+    // which part of the sums this warp puts together: unit group, register, first token group
+    const int my_m = MT == 1 ? 0 : warp >> 2, my_i = warp & 3, my_t = MT == 1 ? warp >> 2 : 0;
+
+    for (int buf = 0;; buf ^= 1) {
+        const int tile = s_next[0], leaf = s_next[1], rows = s_next[2];
+        if (tile >= n_tiles) break;
+        const int groups = (rows + 7) / 8;
+        const int* s_tok = s_tok2 + buf * R;
+        const unsigned char* rec = A.image + leaf * record;
+        if (warp == 0) following = find_tile(tile + gridDim.x);
+
+        // the raw operands of a K-block of 64 outputs, and the outputs' biases
+        struct { uint4 q0, q1, bias; uint2 sc; } next;
+        auto fetch = [&](int u, int kb) {
+            if (u >= units2) return;
+            const uint4* src = reinterpret_cast<const uint4*>(rec + at_w2) + (u * kblocks + kb) * (K16 ? 32 : 64) + lane;
+            const unsigned char* sp = rec + at_s2 + (u * 2 + (g >> 2)) * Kp + kb * 32 + (K16 ? 4 : 8) * c;
+            next.q0 = __ldg(src);
+            if constexpr (K16) {
+                next.sc.x = __ldg(reinterpret_cast<const uint32_t*>(sp));
+            } else {
+                next.q1 = __ldg(src + 32);
+                next.sc = __ldg(reinterpret_cast<const uint2*>(sp));
+            }
+            if (kb == 0 && u * kMxUnit + 8 * g < O)        // (to the end of 16 bytes: records are padded)
+                next.bias = __ldg(reinterpret_cast<const uint4*>(rec + at_b2) + u * 8 + g);
+        };
 
         // ---- hidden values
-        for (int unit0 = 0; unit0 < l; unit0 += 8 * NT) {
-            for (int m0 = 0; m0 < rows; m0 += 32) {
-                int tok[4];
+        for (int unit0 = 0; unit0 < l; unit0 += 16 * MT) {
+            const bool last_pass = !kWide || unit0 + 16 * MT >= l;
+            const int my_unit = unit0 + 16 * my_m + g + 8 * (my_i >> 1);
+            const float my_bias = my_unit < l ? __bfloat162float(__ldg(reinterpret_cast<const __nv_bfloat16*>(rec + at_b1) + my_unit)) : 0.0f;
+            float acc[kMxMaxGroups][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tok[i] = m0 + 8 * i + g < A.tile_rows ? s_tok[m0 + 8 * i + g] : -1;
-                float acc[2][NT][4];
-                mx_hidden<NT, kBig>(A, w1, s1, tok, unit0, warp, lane, acc);
+            for (int t = 0; t < kMxMaxGroups; ++t)
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                for (int i = 0; i < 4; ++i) acc[t][i] = 0.0f;
+            for (int ch = 0; ch < chunks; ++ch) {
+                const int k0 = ch * chunk, ub = k0 / kMxUnit, u0 = ub + warp % kSplit, u1 = min(units1, ub + chunk / kMxUnit);
+                const int row0 = unit0 + 16 * (warp / kSplit);
+                MxCodes q;
 #pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) red[((warp * 2 + m) * NT * 4 + j * 4 + i) * 32 + lane] = acc[m][j][i];
-                __syncthreads();
-                with_activation(A.act, [&](auto act) {
-#pragma unroll
-                    for (int e = 0; e < NT; ++e) {
-                        const int f = warp + kMxWarps * e;             // m-tile, group, register; the lane is the lane
-                        const int m = f / (NT * 4), j = (f >> 2) % NT, i = f & 3;
-                        float sum = 0.0f;
-#pragma unroll
-                        for (int w = 0; w < kMxWarps; ++w) sum += red[(w * 2 * NT * 4 + f) * 32 + lane];
-                        const int unit = unit0 + 8 * j + 2 * c + (i & 1), row = m0 + 16 * m + g + 8 * (i >> 1);
-                        float h = 0.0f;
-                        if (unit < l) h = activate(decltype(act)::value, sum + __bfloat162float(A.b1[(int64_t)leaf * l + unit]));
-                        const float hi = __bfloat162float(__float2bfloat16_rn(h));
-                        hid[row * Kp + unit] = __float2bfloat16_rn(h);
-                        hid[plane + row * Kp + unit] = __float2bfloat16_rn(isinf(hi) ? 0.0f : h - hi);
+                for (int k = 0; k < kMxAhead; ++k) mx_fetch_codes(rec, at_s1, l, row0, u0 + k * kSplit, u1, lane, q, k);
+                const bool fresh = unit0 == 0 || chunks > 1;           // (one chunk stays for all passes)
+                if (ch > 0 || (unit0 > 0 && chunks > 1)) {             // (the first chunk of the first pass is on its way)
+                    __syncthreads();
+                    if (bulk && warp == 0) send_x(mine, k0);
+                }
+                if (fresh && bulk) {
+                    if (!timed_out && !ptx::mbar_wait(&s_full, phase)) timed_out = true;
+                    phase ^= 1;
+                } else if (fresh) {
+                    const int n = min(chunk, D - k0);
+                    for (int r = warp; r < rows; r += NW) {
+                        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(xs + r * pitch);
+                        for (int k = lane; k < n; k += 32) to[k] = A.x[(int64_t)s_tok[r] * D + k0 + k];
+                        // (the last chunk's columns past D)
+                        if (chunks > 1)
+                            for (int k = n + lane; k < chunk; k += 32) to[k] = __float2bfloat16_rn(0.0f);
                     }
-                });
-                __syncthreads();
+                    __syncthreads();
+                }
+                mx_hidden<kBig>(rec, at_s1, l, q, xs, pitch, groups, row0, u0, u1, kSplit, ub, lane, acc);
             }
+#pragma unroll
+            for (int t = 0; t < kMxMaxGroups; ++t) {
+                if (t >= groups) break;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) red[((warp * groups + t) * 4 + i) * 32 + lane] = acc[t][i];
+            }
+            __syncthreads();
+            if (last_pass) {
+                if (warp == 0) announce(following, buf ^ 1);
+                fetch(warp, 0);
+            }
+            with_activation(A.act, [&](auto act) {
+                const float* from = red + (my_m * kSplit * groups * 4 + my_i) * 32 + lane;
+                __nv_bfloat16* to = hid + (2 * c + (my_i & 1)) * Kp + my_unit;
+#pragma unroll 2
+                for (int t = my_t; t < groups; t += MT == 1 ? 2 : 1) {
+                    float sum = my_bias;
+#pragma unroll
+                    for (int w = 0; w < kSplit; ++w) sum += from[(w * groups + t) * 128];
+                    float h = activate_bf16(decltype(act)::value, sum);
+                    if (my_unit >= l) h = 0.0f;
+                    const __nv_bfloat16 hi = __float2bfloat16_rn(h);
+                    const float f = __bfloat162float(hi);
+                    to[8 * t * Kp] = hi;
+                    to[(R + 8 * t) * Kp] = __float2bfloat16_rn(isinf(f) ? 0.0f : h - f);
+                }
+            });
+            __syncthreads();
         }
 
         // ---- outputs
-        for (int u = warp; u < units2; u += kMxWarps) {
-            const int o = u * kMxUnit + 16 * c, n = O - o;
-            uint32_t bias[8];
-            mx_load16(A.b2 + (int64_t)leaf * O + o, n, O % 8 == 0 ? 16 : 2, bias);
-            uint32_t b[8][K16 ? 2 : 4];
-            auto operands = [&](int kb) {
-                uint4 word[2];
-                uint2 sc = make_uint2(0u, 0u);
-                const uint4* src = reinterpret_cast<const uint4*>(w2) + ((int64_t)u * kblocks + kb) * (K16 ? 32 : 64) + lane;
-                word[0] = __ldg(src);
-                word[1] = K16 ? make_uint4(0u, 0u, 0u, 0u) : __ldg(src + 32);
-                const uint8_t* sp = s2 + ((int64_t)u * 2 + (g >> 2)) * Kp + kb * 32 + (K16 ? 4 : 8) * c;
-                if (K16) sc.x = __ldg(reinterpret_cast<const uint32_t*>(sp));
-                else sc = __ldg(reinterpret_cast<const uint2*>(sp));
-                mx_output_operands<K16, kBig>(word, sc, b);
+        for (int u = warp; u < units2; u += NW) {
+            const int o = u * kMxUnit + 8 * g, n = O - o;
+            uint4 bias = next.bias;
+            uint32_t w[8][P];                              // [2 i + row][pair of hidden units]
+            auto operands = [&]() {
+                uint32_t f1[P], f2[P];                     // the scales of a pair of hidden units are neighbouring bytes
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const uint32_t two = p < 2 ? next.sc.x : next.sc.y, lo = (two >> (16 * (p & 1))) & 0xffu, hi = (two >> (16 * (p & 1) + 8)) & 0xffu;
+                    f1[p] = mx_pair(mx_mul1(lo, kBig), mx_mul1(hi, kBig));
+                    f2[p] = kBig ? mx_pair(mx_mul2(lo), mx_mul2(hi)) : 0u;
+                }
+                const uint32_t q[8] = {next.q0.x, next.q0.y, next.q0.z, next.q0.w, next.q1.x, next.q1.y, next.q1.z, next.q1.w};
+#pragma unroll
+                for (int i = 0; i < (K16 ? 4 : 8); ++i) {
+                    uint32_t r[4];
+                    mx_expand(q[i], r);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int row = K16 ? 2 * i + (k >> 1) : i, p = K16 ? k & 1 : k;
+                        w[row][p] = mul_bf16x2(r[k], f1[p]);
+                        if (kBig) w[row][p] = mul_bf16x2(w[row][p], f2[p]);
+                    }
+                }
             };
-            if (kblocks == 1) operands(0);
-            for (int m0 = 0; m0 < rows; m0 += 16) {
-                float acc[8][4];
+            if (!kWide) {
+                operands();
+                fetch(u + NW, 0);
+            }
+            // two token groups at a time: wider leaves expand every K-block once for both
+            constexpr int TG = 2;
+            for (int t0 = 0; t0 < groups; t0 += TG) {
+                float acc[TG][4][4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int t = 0; t < TG; ++t)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[i][k] = 0.0f;
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[t][i][k] = 0.0f;
                 for (int kb = 0; kb < kblocks; ++kb) {
-                    if (kblocks > 1) operands(kb);
+                    if (kWide) {
+                        operands();
+                        if (kb + 1 < kblocks) fetch(u, kb + 1);
+                        else fetch(t0 + TG < groups ? u : u + NW, 0);
+                    }
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        const __nv_bfloat16* h0 = hid + p * plane + (m0 + g) * Kp + kb * 32 + (K16 ? 4 : 8) * c;
-                        if constexpr (K16) {
-                            const uint2 a = *reinterpret_cast<const uint2*>(h0), d = *reinterpret_cast<const uint2*>(h0 + 8 * Kp);
+                    for (int t = 0; t < TG; ++t) {
+                        if (t0 + t >= groups) break;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) ptx::mma_bf16(acc[i], a.x, d.x, a.y, d.y, b[i][0], b[i][1]);
-                        } else {
-                            const uint4 a = *reinterpret_cast<const uint4*>(h0), d = *reinterpret_cast<const uint4*>(h0 + 8 * Kp);
+                        for (int p = 0; p < 2; ++p) {
+                            const __nv_bfloat16* h = hid + (p * R + 8 * (t0 + t) + g) * Kp + kb * 32 + (K16 ? 4 : 8) * c;
+                            if constexpr (K16) {
+                                const uint2 b = *reinterpret_cast<const uint2*>(h);
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                ptx::mma_bf16(acc[i], a.x, d.x, a.y, d.y, b[i][0], b[i][1]);
-                                ptx::mma_bf16(acc[i], a.z, d.z, a.w, d.w, b[i][2], b[i][3]);
+                                for (int i = 0; i < 4; ++i) ptx::mma_bf16(acc[t][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b.x, b.y);
+                            } else {
+                                const uint4 b = *reinterpret_cast<const uint4*>(h);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) ptx::mma_bf16(acc[t][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b.x, b.y);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) ptx::mma_bf16(acc[t][i], w[2 * i][2], w[2 * i + 1][2], w[2 * i][3], w[2 * i + 1][3], b.z, b.w);
                             }
                         }
                     }
                 }
+                const uint32_t bw[4] = {bias.x, bias.y, bias.z, bias.w};
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int tok = s_tok[m0 + g + 8 * r];
-                    uint32_t out[8];
+                for (int t = 0; t < TG; ++t) {
+                    if (t0 + t >= groups) break;
+                    const int2 tok = *reinterpret_cast<const int2*>(s_tok + 8 * (t0 + t) + 2 * c);
+                    uint32_t out[2][4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        out[i] = ptx::pack_bf16(acc[i][2 * r] + __uint_as_float(bias[i] << 16), acc[i][2 * r + 1] + __uint_as_float(bias[i] & 0xffff0000u));
-                    if (tok >= 0) mx_store16(A.y + (int64_t)tok * O + o, n, A.y_bytes, out);
+                    for (int i = 0; i < 4; ++i) {
+                        // (both tokens at once: outputs 2 i and 2 i + 1 of tokens 2 c and 2 c + 1)
+                        float a0, a1, b0, b1;
+                        unpack2(add2(pack2(acc[t][i][0], acc[t][i][1]), splat2(__uint_as_float(bw[i] << 16))), a0, a1);
+                        unpack2(add2(pack2(acc[t][i][2], acc[t][i][3]), splat2(__uint_as_float(bw[i] & 0xffff0000u))), b0, b1);
+                        out[0][i] = ptx::pack_bf16(a0, b0);
+                        out[1][i] = ptx::pack_bf16(a1, b1);
+                    }
+                    if (tok.x >= 0) mx_store8(A.y + (int64_t)tok.x * O + o, n, A.y_bytes == 16, out[0]);
+                    if (tok.y >= 0) mx_store8(A.y + (int64_t)tok.y * O + o, n, A.y_bytes == 16, out[1]);
                 }
             }
         }
+        if (warp == 0) {
+            mine = following;
+            if (lane == 0) { s_next[0] = mine.tile; s_next[1] = mine.leaf; s_next[2] = mine.rows; }
+        }
         __syncthreads();
+    }
+    if (timed_out) {
+        if (lane == 0) atomicExch(A.status, kDevTimeout);
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);     // let bulk copies still in flight land before exit
     }
     // the last CTA to finish clears the counts (and the word behind them that counts the CTAs) for the next call
     if (A.counts) {
-        __shared__ int s_last;
         __syncthreads();
         if (tid == 0) {
             __threadfence();
@@ -602,7 +747,7 @@ k_leaf_mx4(const MxLeafArgs A)
         }
         __syncthreads();
         if (s_last)
-            for (int b = tid; b <= A.n_leaves; b += kMxThreads) A.counts[b] = 0;
+            for (int b = tid; b <= A.n_leaves; b += kThreads) A.counts[b] = 0;
     }
 }
 
@@ -611,9 +756,7 @@ k_leaf_mx4(const MxLeafArgs A)
 struct MxRowsArgs {
     const __nv_bfloat16* x;
     const int32_t *leaf_idx, *perm;    // perm nullptr: in order
-    const uint32_t *w1, *w2;
-    const uint8_t *s1, *s2;
-    const __nv_bfloat16 *b1, *b2;
+    const unsigned char* image;
     __nv_bfloat16* y;
     MxLayout lay;
     int act;
@@ -656,6 +799,7 @@ k_leaf_mx4_rows(const MxRowsArgs A)
     const MxLayout& Ly = A.lay;
     const int lane = threadIdx.x & 31, wib = threadIdx.x >> 5, D = Ly.D, O = Ly.O, l = Ly.l;
     const int wd = (D + 7) / 8, wo = (O + 7) / 8, nd = (int)mx_scales(D), no = (int)mx_scales(O);
+    const int64_t record = Ly.record();
     float* h = s_mxh + (size_t)wib * l;
     auto load8 = [&](const __nv_bfloat16* p, int n, bool vec, float (&v)[8]) {
         if (vec) {
@@ -681,8 +825,11 @@ k_leaf_mx4_rows(const MxRowsArgs A)
         } else {
             j = A.leaf_idx[t];
         }
-        const uint32_t *w1 = A.w1 + j * l * wd, *w2 = A.w2 + j * l * wo;
-        const uint8_t *s1 = A.s1 + j * l * nd, *s2 = A.s2 + j * l * no;
+        const unsigned char* rec = A.image + j * record;
+        if (lane == 0) mx_prefetch(rec, record);
+        const uint32_t *w1 = reinterpret_cast<const uint32_t*>(rec), *w2 = reinterpret_cast<const uint32_t*>(rec + Ly.at_w2());
+        const uint8_t *s1 = rec + Ly.at_s1(), *s2 = rec + Ly.at_s2();
+        const __nv_bfloat16 *b1 = reinterpret_cast<const __nv_bfloat16*>(rec + Ly.at_b1()), *b2 = reinterpret_cast<const __nv_bfloat16*>(rec + Ly.at_b2());
         for (int i0 = 0; i0 < l; i0 += U) {
             float acc[U] = {};
             for (int w = lane; w < wd; w += 32) {
@@ -700,14 +847,14 @@ k_leaf_mx4_rows(const MxRowsArgs A)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const float sum = warp_sum(acc[u]);
-                if (lane == 0 && i0 + u < l) h[i0 + u] = activate(A.act, sum + __bfloat162float(A.b1[j * l + i0 + u]));
+                if (lane == 0 && i0 + u < l) h[i0 + u] = activate(A.act, sum + __bfloat162float(b1[i0 + u]));
             }
         }
         __syncwarp();
         __nv_bfloat16* yt = A.y + t * O;
         for (int w = lane; w < wo; w += 32) {
             float acc[8];
-            load8(A.b2 + j * O + 8 * w, O - 8 * w, A.y_vec, acc);
+            load8(b2 + 8 * w, O - 8 * w, true, acc);
             for (int q = 0; q < l; ++q) {
                 float v[8];
                 mx_floats(__ldg(w2 + (int64_t)q * wo + w), __ldg(s2 + q * no + (w >> 2)), A.big, v);

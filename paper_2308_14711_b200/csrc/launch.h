@@ -56,30 +56,31 @@ cudaError_t quantize_mx4(const LaunchOn& on, const void* src, int elem_bytes, in
 cudaError_t dequantize_mx4(const LaunchOn& on, const uint8_t* codes, const uint8_t* scales, int elem_bytes, int64_t rows, int64_t cols,
                            void* values);
 
-// A layer's images (all owned by its handle).
+// A layer's image (owned by its handle).
 struct Mx4Layer {
-    uint32_t *w1 = nullptr, *w2 = nullptr;
-    uint8_t *s1 = nullptr, *s2 = nullptr;
+    unsigned char* image = nullptr;
     int D = 0, O = 0, l = 0;
     bool mma = false;             // leaves wide enough for the tensor-core kernel
     bool big = false;             // some scale is over 2
 };
-struct Mx4Bytes { size_t w1, s1, w2, s2; };      // of the images
 bool mx4_on_tensor_cores(int leaf_width);
 constexpr int kMx4MaxLeafWidth = 1024;           // hidden values of a tile are kept in shared memory
-Mx4Bytes mx4_image_bytes(const Mx4Layer& m, int64_t n_leaves);
+size_t mx4_image_bytes(const Mx4Layer& m, int64_t n_leaves);
+bool mx4_record_fits(const Mx4Layer& m);          // offsets inside a leaf's record are ints
 // flag: one int of device memory, zero; set where a scale is over 2.
 cudaError_t mx4_find_big(const uint8_t* scales, int64_t n, int* flag, int sm_count);
-cudaError_t mx4_pack(const Mx4Layer& m, const uint8_t* w1, const uint8_t* s1, const uint8_t* w2, const uint8_t* s2, int64_t n_leaves,
-                     int sm_count);
+cudaError_t mx4_pack(const Mx4Layer& m, const uint8_t* w1, const uint8_t* s1, const uint8_t* w2, const uint8_t* s2, const void* b1,
+                     const void* b2, int64_t n_leaves, int sm_count);
 
 // The leaf kernels.  tiles / n_tiles: a tile list over perm; counts != nullptr: perm is the table of lists [n_leaves][cap] instead.
 struct Mx4Tokens {
     const void *x;
     void *y;
-    const void *b1, *b2;
     int act;
+    int* status;
 };
+// Rows of the largest tile worth having; lists of up to n_leaves leaves.
+int mx4_most_rows(const Mx4Layer& m, int n_leaves);
 cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* perm, const void* tiles, int n_tiles,
                            int tile_rows, int32_t* counts, int n_leaves, int cap);
 // The tail of the walk (levels > 0) as in k_leaf_warp.

@@ -15,11 +15,11 @@ std::mutex g_mu;
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// Widest access to 16 consecutive elements at a multiple of 16 in rows of `cols` bf16 values: 32, 16 or 2 bytes.
-int access_bytes(const void* p, int cols) {
-    if (cols % 16 == 0 && aligned(p, 32)) return 32;
-    return cols % 8 == 0 && aligned(p, 16) ? 16 : 2;
-}
+// Widest access to 8 consecutive elements at a multiple of 8 in rows of `cols` bf16 values.
+int access_bytes(const void* p, int cols) { return cols % 8 == 0 && aligned(p, 16) ? 16 : 2; }
+
+constexpr int kMxSmemMost = 226 * 1024;                       // shared memory of a CTA that has an SM to itself, or shares it with another
+constexpr int kMxSmemPair = (227 * 1024) / 2 - 1024 - 128;
 
 MxLayout layout(const Mx4Layer& m) { return MxLayout{m.D, m.O, m.l, m.mma}; }
 
@@ -42,21 +42,21 @@ cudaError_t dequantize(const LaunchOn& on, const uint8_t* codes, const uint8_t* 
                      rows, cols);
 }
 
-template <int NT, bool kBig>
+template <int MT, bool kWide, bool kBig>
 cudaError_t launch_tiles(const LaunchOn& on, const MxLeafArgs& a, int n_tiles) {
-    const int smem = MxLeafSmem<NT>::bytes(a.tile_rows, a.lay.Kp(), a.counts ? a.n_leaves : 0);
+    const int smem = MxLeafSmem{a.tile_rows, a.lay.D, a.lay.Kp(), a.counts ? a.n_leaves : 0}.bytes();
     static bool raised[kMaxDevices] = {};
     {
         std::lock_guard<std::mutex> lk(g_mu);
         if (!raised[on.device]) {
-            const cudaError_t e = cudaFuncSetAttribute(k_leaf_mx4<NT, kBig>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+            const cudaError_t e = cudaFuncSetAttribute(k_leaf_mx4<MT, kWide, kBig>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxSmemMost);
             if (e != cudaSuccess) return e;
             raised[on.device] = true;
         }
     }
-    const int per_sm = std::max(1, std::min(2, 227 * 1024 / (smem + 1536)));
+    const int per_sm = smem <= kMxSmemPair ? 2 : 1;
     const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>((int64_t)on.sm_count * per_sm, n_tiles));
-    return launch_on(on, k_leaf_mx4<NT, kBig>, grid, 1, kMxThreads, (size_t)smem, a);
+    return launch_on(on, k_leaf_mx4<MT, kWide, kBig>, grid, 1, kMxThreads, (size_t)smem, a);
 }
 
 }  // namespace
@@ -76,9 +76,9 @@ cudaError_t dequantize_mx4(const LaunchOn& on, const uint8_t* codes, const uint8
 // (leaves of fewer than 8 neurons would leave most of an MMA's columns empty)
 bool mx4_on_tensor_cores(int leaf_width) { return leaf_width >= 8; }
 
-Mx4Bytes mx4_image_bytes(const Mx4Layer& m, int64_t n_leaves) {
-    const MxLayout L = layout(m);
-    return Mx4Bytes{(size_t)(L.w1() * n_leaves), (size_t)(L.s1() * n_leaves), (size_t)(L.w2() * n_leaves), (size_t)(L.s2() * n_leaves)};
+size_t mx4_image_bytes(const Mx4Layer& m, int64_t n_leaves) { return (size_t)layout(m).record() * (size_t)n_leaves; }
+bool mx4_record_fits(const Mx4Layer& m) {
+    return ((int64_t)m.l * ((int64_t)m.D + m.O) + 64 * (int64_t)m.l) * 4 < ((int64_t)1 << 30);
 }
 
 cudaError_t mx4_find_big(const uint8_t* scales, int64_t n, int* flag, int sm_count) {
@@ -86,10 +86,17 @@ cudaError_t mx4_find_big(const uint8_t* scales, int64_t n, int* flag, int sm_cou
     return cudaGetLastError();
 }
 
-cudaError_t mx4_pack(const Mx4Layer& m, const uint8_t* w1, const uint8_t* s1, const uint8_t* w2, const uint8_t* s2, int64_t n_leaves,
-                     int sm_count) {
-    k_pack_mx4<<<(unsigned)sm_count * 8, 256>>>(w1, s1, w2, s2, m.w1, m.s1, m.w2, m.s2, layout(m), n_leaves, m.big);
+cudaError_t mx4_pack(const Mx4Layer& m, const uint8_t* w1, const uint8_t* s1, const uint8_t* w2, const uint8_t* s2, const void* b1,
+                     const void* b2, int64_t n_leaves, int sm_count) {
+    k_pack_mx4<<<(unsigned)sm_count * 8, 256>>>(w1, s1, w2, s2, (const uint16_t*)b1, (const uint16_t*)b2, m.image, layout(m), n_leaves, m.big);
     return cudaGetLastError();
+}
+
+// Most tokens (a multiple of 8) that a tile can have while two CTAs fit an SM; 32 at least.
+int mx4_most_rows(const Mx4Layer& m, int n_leaves) {
+    for (int rows = 8 * kMxMaxGroups; rows > 32; rows -= 8)
+        if (MxLeafSmem{rows, m.D, layout(m).Kp(), n_leaves}.bytes() <= kMxSmemPair) return rows;
+    return 32;
 }
 
 cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* perm, const void* tiles, int n_tiles,
@@ -102,17 +109,17 @@ cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Token
     a.counts = counts;
     a.n_leaves = n_leaves;
     a.cap = cap;
-    a.w1 = m.w1; a.w2 = m.w2; a.s1 = m.s1; a.s2 = m.s2;
-    a.b1 = (const __nv_bfloat16*)t.b1;
-    a.b2 = (const __nv_bfloat16*)t.b2;
+    a.image = m.image;
     a.y = (__nv_bfloat16*)t.y;
     a.lay = layout(m);
     a.act = t.act;
     a.tile_rows = tile_rows;
     a.x_bytes = access_bytes(t.x, m.D);
     a.y_bytes = access_bytes(t.y, m.O);
-    if (m.l <= 16) return m.big ? launch_tiles<2, true>(on, a, n_tiles) : launch_tiles<2, false>(on, a, n_tiles);
-    return m.big ? launch_tiles<4, true>(on, a, n_tiles) : launch_tiles<4, false>(on, a, n_tiles);
+    a.status = t.status;
+    if (m.l <= 16) return m.big ? launch_tiles<1, false, true>(on, a, n_tiles) : launch_tiles<1, false, false>(on, a, n_tiles);
+    if (m.l <= 32) return m.big ? launch_tiles<2, false, true>(on, a, n_tiles) : launch_tiles<2, false, false>(on, a, n_tiles);
+    return m.big ? launch_tiles<2, true, true>(on, a, n_tiles) : launch_tiles<2, true, false>(on, a, n_tiles);
 }
 
 cudaError_t mx4_leaf_rows(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* leaf_idx, const int32_t* perm, int64_t B,
@@ -121,9 +128,7 @@ cudaError_t mx4_leaf_rows(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens
     a.x = (const __nv_bfloat16*)t.x;
     a.leaf_idx = leaf_idx;
     a.perm = perm;
-    a.w1 = m.w1; a.w2 = m.w2; a.s1 = m.s1; a.s2 = m.s2;
-    a.b1 = (const __nv_bfloat16*)t.b1;
-    a.b2 = (const __nv_bfloat16*)t.b2;
+    a.image = m.image;
     a.y = (__nv_bfloat16*)t.y;
     a.lay = layout(m);
     a.act = t.act;
