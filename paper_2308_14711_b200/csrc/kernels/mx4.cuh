@@ -379,14 +379,15 @@ struct MxCodes {
     uint2 code[kMxAhead][2];
     uint32_t sc[kMxAhead][2];
 };
+// (Rows past the leaf's last repeat it: their sums are not used.  u past the last unit likewise.)
 __device__ __forceinline__ void mx_fetch_codes(const unsigned char* __restrict__ rec, int at_s1, int l, int row0, int u, int u1, int lane, MxCodes& q, int k) {
     const int g = lane >> 2, c = lane & 3;
+    const int base = min(u, u1 - 1) * l;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int row = row0 + 8 * h + g;
-        const bool in = row < l && u < u1;
-        q.code[k][h] = in ? __ldg(reinterpret_cast<const uint2*>(rec) + (u * l + row) * 4 + c) : make_uint2(0u, 0u);
-        q.sc[k][h] = in ? __ldg(rec + at_s1 + (u * l + row) * 2 + (c >> 1)) : 0u;
+        const int row = base + min(row0 + 8 * h + g, l - 1);
+        q.code[k][h] = __ldg(reinterpret_cast<const uint2*>(rec) + row * 4 + c);
+        q.sc[k][h] = __ldg(rec + at_s1 + row * 2 + (c >> 1));
     }
 }
 template <bool kBig>
@@ -404,14 +405,21 @@ __device__ __forceinline__ void mx_hidden(const unsigned char* __restrict__ rec,
             for (int h = 0; h < 2; ++h) mx_row16<kBig>(q.code[k][h], q.sc[k][h], w[h]);
             if (uk + kMxAhead * step < u1) mx_fetch_codes(rec, at_s1, l, row0, uk + kMxAhead * step, u1, lane, q, k);
             const unsigned char* xp = xs + g * pitch + (uk - unit_base) * (kMxUnit * 2) + 32 * c;
+            // (two groups at a time, whose MMAs do not wait for one another; a last odd group is computed twice)
 #pragma unroll
-            for (int t = 0; t < kMxMaxGroups; ++t) {
+            for (int t = 0; t < kMxMaxGroups; t += 2) {
                 if (t >= groups) break;
-                const uint4 a = *reinterpret_cast<const uint4*>(xp + t * 8 * pitch), b = *reinterpret_cast<const uint4*>(xp + t * 8 * pitch + 16);
-                ptx::mma_bf16(acc[t], w[0][0], w[1][0], w[0][1], w[1][1], a.x, a.y);
-                ptx::mma_bf16(acc[t], w[0][2], w[1][2], w[0][3], w[1][3], a.z, a.w);
-                ptx::mma_bf16(acc[t], w[0][4], w[1][4], w[0][5], w[1][5], b.x, b.y);
-                ptx::mma_bf16(acc[t], w[0][6], w[1][6], w[0][7], w[1][7], b.z, b.w);
+                const unsigned char *xa = xp + t * 8 * pitch, *xb = t + 1 < groups ? xa + 8 * pitch : xa;
+                const uint4 a0 = *reinterpret_cast<const uint4*>(xa), b0 = *reinterpret_cast<const uint4*>(xb);
+                const uint4 a1 = *reinterpret_cast<const uint4*>(xa + 16), b1 = *reinterpret_cast<const uint4*>(xb + 16);
+                ptx::mma_bf16(acc[t], w[0][0], w[1][0], w[0][1], w[1][1], a0.x, a0.y);
+                ptx::mma_bf16(acc[t + 1], w[0][0], w[1][0], w[0][1], w[1][1], b0.x, b0.y);
+                ptx::mma_bf16(acc[t], w[0][2], w[1][2], w[0][3], w[1][3], a0.z, a0.w);
+                ptx::mma_bf16(acc[t + 1], w[0][2], w[1][2], w[0][3], w[1][3], b0.z, b0.w);
+                ptx::mma_bf16(acc[t], w[0][4], w[1][4], w[0][5], w[1][5], a1.x, a1.y);
+                ptx::mma_bf16(acc[t + 1], w[0][4], w[1][4], w[0][5], w[1][5], b1.x, b1.y);
+                ptx::mma_bf16(acc[t], w[0][6], w[1][6], w[0][7], w[1][7], a1.z, a1.w);
+                ptx::mma_bf16(acc[t + 1], w[0][6], w[1][6], w[0][7], w[1][7], b1.z, b1.w);
             }
         }
     }
@@ -448,7 +456,7 @@ k_leaf_mx4(const MxLeafArgs A)
     constexpr int NW = kMxWarps, kThreads = kMxThreads, P = K16 ? 2 : 4;
     constexpr int kSplit = NW / MT;                        // warps that share a group of 16 hidden units
     extern __shared__ __align__(16) unsigned char smem_mx[];
-    __shared__ int s_wsum[NW], s_last, s_next[3];          // s_next: tile, leaf, rows
+    __shared__ int s_wsum[NW], s_last, s_next[2][3];       // s_next: tile, leaf, rows
     __shared__ uint64_t s_full;
     const MxLayout& Ly = A.lay;
     const int l = Ly.l, D = Ly.D, O = Ly.O, Kp = K16 ? 16 : kWide ? Ly.Kp() : 32;
@@ -533,16 +541,18 @@ k_leaf_mx4(const MxLeafArgs A)
     auto announce = [&](const Found& f, int buf) {
         if (lane < R) s_tok2[buf * R + lane] = f.tok[0];
         if (lane + 32 < R) s_tok2[buf * R + lane + 32] = f.tok[1];
+        if (lane == 0) { s_next[buf][0] = f.tile; s_next[buf][1] = f.leaf; s_next[buf][2] = f.rows; }
         if (f.rows > 0) {
             if (bulk) send_x(f, 0);
             if (lane == 0) mx_prefetch(A.image + f.leaf * record, record);
         }
     };
-    Found mine, following;                                 // (warp 0)
-    if (warp == 0) {
+    // The last warp (which has the least to do where units do not come out even) finds the tiles and sends for their rows.
+    constexpr int kFinder = NW - 1;
+    Found mine, following;
+    if (warp == kFinder) {
         mine = find_tile(blockIdx.x);
         announce(mine, 0);
-        if (lane == 0) { s_next[0] = mine.tile; s_next[1] = mine.leaf; s_next[2] = mine.rows; }
     }
     __syncthreads();
     uint32_t phase = 0;
@@ -550,13 +560,16 @@ k_leaf_mx4(const MxLeafArgs A)
     // which part of the sums this warp puts together: unit group, register, first token group
     const int my_m = MT == 1 ? 0 : warp >> 2, my_i = warp & 3, my_t = MT == 1 ? warp >> 2 : 0;
 
+    // Two barriers per tile: one between the partial sums and the hidden values, one between those and the outputs.  A warp that has
+    // written its outputs goes on to the next tile, which the finder announced between the two (sums, hidden values, tokens and the
+    // announcement are not written again before every warp has passed the first barrier of that tile).
     for (int buf = 0;; buf ^= 1) {
-        const int tile = s_next[0], leaf = s_next[1], rows = s_next[2];
+        const int tile = s_next[buf][0], leaf = s_next[buf][1], rows = s_next[buf][2];
         if (tile >= n_tiles) break;
         const int groups = (rows + 7) / 8;
         const int* s_tok = s_tok2 + buf * R;
         const unsigned char* rec = A.image + leaf * record;
-        if (warp == 0) following = find_tile(tile + gridDim.x);
+        if (warp == kFinder) following = find_tile(tile + gridDim.x);
 
         // the raw operands of a K-block of 64 outputs, and the outputs' biases
         struct { uint4 q0, q1, bias; uint2 sc; } next;
@@ -594,10 +607,10 @@ k_leaf_mx4(const MxLeafArgs A)
                 const bool fresh = unit0 == 0 || chunks > 1;           // (one chunk stays for all passes)
                 if (ch > 0 || (unit0 > 0 && chunks > 1)) {             // (the first chunk of the first pass is on its way)
                     __syncthreads();
-                    if (bulk && warp == 0) send_x(mine, k0);
+                    if (bulk && warp == kFinder) send_x(mine, k0);
                 }
                 if (fresh && bulk) {
-                    if (!timed_out && !ptx::mbar_wait(&s_full, phase)) timed_out = true;
+                    if (!timed_out && !ptx::mbar_wait_suspended(&s_full, phase)) timed_out = true;
                     phase ^= 1;
                 } else if (fresh) {
                     const int n = min(chunk, D - k0);
@@ -620,7 +633,7 @@ k_leaf_mx4(const MxLeafArgs A)
             }
             __syncthreads();
             if (last_pass) {
-                if (warp == 0) announce(following, buf ^ 1);
+                if (warp == kFinder) announce(following, buf ^ 1);
                 fetch(warp, 0);
             }
             with_activation(A.act, [&](auto act) {
@@ -645,7 +658,16 @@ k_leaf_mx4(const MxLeafArgs A)
         // ---- outputs
         for (int u = warp; u < units2; u += NW) {
             const int o = u * kMxUnit + 8 * g, n = O - o;
-            uint4 bias = next.bias;
+            // biases as the sums that the MMAs start from: outputs 2 i and 2 i + 1 of two tokens
+            float bias[4][4];
+            {
+                const uint32_t bw[4] = {next.bias.x, next.bias.y, next.bias.z, next.bias.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    bias[i][0] = bias[i][1] = __uint_as_float(bw[i] << 16);
+                    bias[i][2] = bias[i][3] = __uint_as_float(bw[i] & 0xffff0000u);
+                }
+            }
             uint32_t w[8][P];                              // [2 i + row][pair of hidden units]
             auto operands = [&]() {
                 uint32_t f1[P], f2[P];                     // the scales of a pair of hidden units are neighbouring bytes
@@ -672,16 +694,21 @@ k_leaf_mx4(const MxLeafArgs A)
                 operands();
                 fetch(u + NW, 0);
             }
-            // two token groups at a time: wider leaves expand every K-block once for both
+            // two token groups at a time, whose MMAs do not wait for one another (a last odd group is computed twice); wider leaves expand
+            // every K-block once for both
             constexpr int TG = 2;
             for (int t0 = 0; t0 < groups; t0 += TG) {
                 float acc[TG][4][4];
+                if constexpr (kWide) {
 #pragma unroll
-                for (int t = 0; t < TG; ++t)
+                    for (int t = 0; t < TG; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) acc[t][i][k] = 0.0f;
+                            for (int k = 0; k < 4; ++k) acc[t][i][k] = bias[i][k];
+                }
+                const __nv_bfloat16* ha = hid + (8 * t0 + g) * Kp + (K16 ? 4 : 8) * c;
+                const __nv_bfloat16* hb = t0 + 1 < groups ? ha + 8 * Kp : ha;
                 for (int kb = 0; kb < kblocks; ++kb) {
                     if (kWide) {
                         operands();
@@ -689,50 +716,56 @@ k_leaf_mx4(const MxLeafArgs A)
                         else fetch(t0 + TG < groups ? u : u + NW, 0);
                     }
 #pragma unroll
-                    for (int t = 0; t < TG; ++t) {
-                        if (t0 + t >= groups) break;
+                    for (int p = 0; p < 2; ++p) {
+                        if constexpr (K16) {
+                            const uint2 b0 = *reinterpret_cast<const uint2*>(ha + p * R * Kp), b1 = *reinterpret_cast<const uint2*>(hb + p * R * Kp);
 #pragma unroll
-                        for (int p = 0; p < 2; ++p) {
-                            const __nv_bfloat16* h = hid + (p * R + 8 * (t0 + t) + g) * Kp + kb * 32 + (K16 ? 4 : 8) * c;
-                            if constexpr (K16) {
-                                const uint2 b = *reinterpret_cast<const uint2*>(h);
+                            for (int i = 0; i < 4; ++i) {
+                                if (p == 0) {
+                                    ptx::mma_bf16_from(acc[0][i], bias[i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b0.x, b0.y);
+                                    ptx::mma_bf16_from(acc[1][i], bias[i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b1.x, b1.y);
+                                } else {
+                                    ptx::mma_bf16(acc[0][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b0.x, b0.y);
+                                    ptx::mma_bf16(acc[1][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b1.x, b1.y);
+                                }
+                            }
+                        } else {
+                            const uint4 b0 = *reinterpret_cast<const uint4*>(ha + p * R * Kp + kb * 32);
+                            const uint4 b1 = *reinterpret_cast<const uint4*>(hb + p * R * Kp + kb * 32);
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) ptx::mma_bf16(acc[t][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b.x, b.y);
-                            } else {
-                                const uint4 b = *reinterpret_cast<const uint4*>(h);
+                            for (int i = 0; i < 4; ++i) {
+                                if (!kWide && p == 0) {
+                                    ptx::mma_bf16_from(acc[0][i], bias[i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b0.x, b0.y);
+                                    ptx::mma_bf16_from(acc[1][i], bias[i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b1.x, b1.y);
+                                } else {
+                                    ptx::mma_bf16(acc[0][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b0.x, b0.y);
+                                    ptx::mma_bf16(acc[1][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b1.x, b1.y);
+                                }
+                            }
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) ptx::mma_bf16(acc[t][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b.x, b.y);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) ptx::mma_bf16(acc[t][i], w[2 * i][2], w[2 * i + 1][2], w[2 * i][3], w[2 * i + 1][3], b.z, b.w);
+                            for (int i = 0; i < 4; ++i) {
+                                ptx::mma_bf16(acc[0][i], w[2 * i][2], w[2 * i + 1][2], w[2 * i][3], w[2 * i + 1][3], b0.z, b0.w);
+                                ptx::mma_bf16(acc[1][i], w[2 * i][2], w[2 * i + 1][2], w[2 * i][3], w[2 * i + 1][3], b1.z, b1.w);
                             }
                         }
                     }
                 }
-                const uint32_t bw[4] = {bias.x, bias.y, bias.z, bias.w};
 #pragma unroll
                 for (int t = 0; t < TG; ++t) {
                     if (t0 + t >= groups) break;
                     const int2 tok = *reinterpret_cast<const int2*>(s_tok + 8 * (t0 + t) + 2 * c);
-                    uint32_t out[2][4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        // (both tokens at once: outputs 2 i and 2 i + 1 of tokens 2 c and 2 c + 1)
-                        float a0, a1, b0, b1;
-                        unpack2(add2(pack2(acc[t][i][0], acc[t][i][1]), splat2(__uint_as_float(bw[i] << 16))), a0, a1);
-                        unpack2(add2(pack2(acc[t][i][2], acc[t][i][3]), splat2(__uint_as_float(bw[i] & 0xffff0000u))), b0, b1);
-                        out[0][i] = ptx::pack_bf16(a0, b0);
-                        out[1][i] = ptx::pack_bf16(a1, b1);
+                    for (int r = 0; r < 2; ++r) {
+                        const int to = r ? tok.y : tok.x;
+                        uint32_t out[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) out[i] = ptx::pack_bf16(acc[t][i][r], acc[t][i][2 + r]);
+                        if (to >= 0) mx_store8(A.y + (int64_t)to * O + o, n, A.y_bytes == 16, out);
                     }
-                    if (tok.x >= 0) mx_store8(A.y + (int64_t)tok.x * O + o, n, A.y_bytes == 16, out[0]);
-                    if (tok.y >= 0) mx_store8(A.y + (int64_t)tok.y * O + o, n, A.y_bytes == 16, out[1]);
                 }
             }
         }
-        if (warp == 0) {
-            mine = following;
-            if (lane == 0) { s_next[0] = mine.tile; s_next[1] = mine.leaf; s_next[2] = mine.rows; }
-        }
-        __syncthreads();
+        mine = following;
     }
     if (timed_out) {
         if (lane == 0) atomicExch(A.status, kDevTimeout);
