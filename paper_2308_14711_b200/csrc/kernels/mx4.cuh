@@ -36,9 +36,44 @@ __device__ __forceinline__ int mx_block_scale(unsigned a) { return a >= 0x7f8000
 
 template <typename T> __device__ __forceinline__ float load_float(const T* p) { return Elem<T>::to_float(*p); }
 
-// Eight elements per thread, four threads per block.  Whole: rows of whole blocks, i.e. one long run of 16-byte vectors;
-// otherwise rows start anywhere and end inside a block.  Bound: HBM.
-template <typename T, bool kWhole>
+// How rows lie: whole blocks, i.e. one long run of 16-byte vectors; whole groups of eight columns, so that vectors start everywhere but
+// blocks may be cut; anything.
+enum : int { kMxWhole = 0, kMxGroups = 1, kMxAny = 2 };
+
+// unit / d and its remainder; 32-bit where the numbers are (a 64-bit division is a call of 100 instructions).
+__device__ __forceinline__ int64_t mx_divide(int64_t unit, uint32_t d, bool small, uint32_t& rest) {
+    if (small) {
+        const uint32_t q = (uint32_t)unit / d;
+        rest = (uint32_t)unit - q * d;
+        return q;
+    }
+    const int64_t q = unit / d;
+    rest = (uint32_t)(unit - q * d);
+    return q;
+}
+
+// The values of a word's first n codes.
+template <typename T, int kRows>
+__device__ __forceinline__ void mx_write_values(T* __restrict__ to, uint32_t word, float scale, int n) {
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = mx_code_value(word >> (4 * e)) * scale;
+    if constexpr (kRows != kMxAny && sizeof(T) == 2) {
+        uint4 q;
+        q.x = ptx::pack_bf16(o[0], o[1]); q.y = ptx::pack_bf16(o[2], o[3]); q.z = ptx::pack_bf16(o[4], o[5]); q.w = ptx::pack_bf16(o[6], o[7]);
+        __stcs(reinterpret_cast<uint4*>(to), q);
+    } else if constexpr (kRows != kMxAny) {
+        __stcs(reinterpret_cast<float4*>(to), make_float4(o[0], o[1], o[2], o[3]));
+        __stcs(reinterpret_cast<float4*>(to) + 1, make_float4(o[4], o[5], o[6], o[7]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n) to[e] = Elem<T>::from_float(o[e]);
+    }
+}
+
+// Eight elements per thread, four threads per block.  Bound: HBM.
+template <typename T, int kRows>
 __global__ void __launch_bounds__(256)
 k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, T* __restrict__ values, int64_t rows,
                int64_t cols)
@@ -47,22 +82,26 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
     pdl_wait();
     const int64_t nb = mx_scales(cols), cb = mx_code_bytes(cols), total = rows * nb * 4;
     const int64_t step = (int64_t)gridDim.x * blockDim.x;
+    const bool small = total + 4 * step < ((int64_t)1 << 31);
     constexpr int U = 2;                                   // groups whose loads are in flight
-    // (whole warps: the shuffles below want all lanes; U * step is a multiple of 32, and so is the rounded total)
+    // (whole warps: the shuffles below want all lanes; step is a multiple of 32, and so is the rounded total)
     const int64_t end = (total + 31) & ~(int64_t)31;
     for (int64_t u0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u0 < end; u0 += U * step) {
         float v[U][8];
-        int64_t at[U];
+        int64_t at[U], row[U];
+        uint32_t g[U];                                     // group of the row
         int n[U];                                          // elements of the group that exist
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t unit = u0 + u * step;
-            const int64_t row = kWhole ? 0 : unit / (nb * 4), c0 = kWhole ? unit * 8 : (unit - row * nb * 4) * 8;
-            n[u] = unit < total ? (kWhole ? 8 : (int)max((int64_t)0, min((int64_t)8, cols - c0))) : 0;
-            at[u] = kWhole ? c0 : row * cols + c0;
+            row[u] = 0;
+            g[u] = 0;
+            if (kRows != kMxWhole) row[u] = mx_divide(unit, (uint32_t)(nb * 4), small, g[u]);
+            n[u] = unit >= total ? 0 : kRows == kMxWhole ? 8 : (int)max((int64_t)0, min((int64_t)8, cols - (int64_t)g[u] * 8));
+            at[u] = kRows == kMxWhole ? unit * 8 : row[u] * cols + (int64_t)g[u] * 8;
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[u][e] = 0.0f;
-            if (kWhole) {
+            if (kRows != kMxAny) {
                 if (n[u]) {
                     if constexpr (sizeof(T) == 2) {
                         Elem<T>::load_vec(src + at[u], v[u]);
@@ -97,68 +136,38 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
                 word |= (uint32_t)__nv_cvt_float2_to_fp4x2(q, __NV_E2M1, cudaRoundNearest) << (4 * e);
             }
             if (n[u] == 0) continue;
-            const int64_t row = kWhole ? 0 : unit / (nb * 4), g = kWhole ? unit : unit - row * nb * 4;
-            if constexpr (kWhole) {
-                *reinterpret_cast<uint32_t*>(codes + unit * 4) = word;
+            if constexpr (kRows != kMxAny) {
+                *reinterpret_cast<uint32_t*>(codes + (kRows == kMxWhole ? unit * 4 : row[u] * cb + (int64_t)g[u] * 4)) = word;
             } else {
-                uint8_t* to = codes + row * cb + g * 4;
+                uint8_t* to = codes + row[u] * cb + (int64_t)g[u] * 4;
                 for (int e = 0; e < n[u]; e += 2) to[e >> 1] = (uint8_t)(word >> (4 * e));
             }
-            if ((g & 3) == 0) scales[kWhole ? unit >> 2 : row * nb + (g >> 2)] = (uint8_t)s;
-            if (values) {
-                const float sc = mx_scale(s);
-                float o[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = mx_code_value(word >> (4 * e)) * sc;
-                if constexpr (kWhole && sizeof(T) == 2) {
-                    uint4 q;
-                    q.x = ptx::pack_bf16(o[0], o[1]); q.y = ptx::pack_bf16(o[2], o[3]); q.z = ptx::pack_bf16(o[4], o[5]); q.w = ptx::pack_bf16(o[6], o[7]);
-                    __stcs(reinterpret_cast<uint4*>(values + at[u]), q);
-                } else if constexpr (kWhole) {
-                    __stcs(reinterpret_cast<float4*>(values + at[u]), make_float4(o[0], o[1], o[2], o[3]));
-                    __stcs(reinterpret_cast<float4*>(values + at[u]) + 1, make_float4(o[4], o[5], o[6], o[7]));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (e < n[u]) values[at[u] + e] = Elem<T>::from_float(o[e]);
-                }
-            }
+            if (((kRows == kMxWhole ? (uint32_t)unit : g[u]) & 3) == 0) scales[kRows == kMxWhole ? unit >> 2 : row[u] * nb + (g[u] >> 2)] = (uint8_t)s;
+            if (values) mx_write_values<T, kRows>(values + at[u], word, mx_scale(s), n[u]);
         }
     }
 }
 
-template <typename T, bool kWhole>
+template <typename T, int kRows>
 __global__ void __launch_bounds__(256)
 k_dequantize_mx4(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, T* __restrict__ values, int64_t rows, int64_t cols)
 {
     pdl_trigger();
     pdl_wait();
     const int64_t nb = mx_scales(cols), cb = mx_code_bytes(cols), total = rows * nb * 4;
-    for (int64_t unit = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; unit < total; unit += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t row = kWhole ? 0 : unit / (nb * 4), g = kWhole ? unit : unit - row * nb * 4;
-        const int n = kWhole ? 8 : (int)max((int64_t)0, min((int64_t)8, cols - g * 8));
+    const int64_t step = (int64_t)gridDim.x * blockDim.x;
+    const bool small = total + 4 * step < ((int64_t)1 << 31);
+    for (int64_t unit = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; unit < total; unit += step) {
+        uint32_t g = 0;
+        const int64_t row = kRows == kMxWhole ? 0 : mx_divide(unit, (uint32_t)(nb * 4), small, g);
+        const int n = kRows == kMxWhole ? 8 : (int)max((int64_t)0, min((int64_t)8, cols - (int64_t)g * 8));
         if (n == 0) continue;
         uint32_t word = 0;
-        if constexpr (kWhole) word = __ldcs(reinterpret_cast<const uint32_t*>(codes + unit * 4));
+        if constexpr (kRows != kMxAny) word = __ldcs(reinterpret_cast<const uint32_t*>(codes + (kRows == kMxWhole ? unit * 4 : row * cb + (int64_t)g * 4)));
         else
-            for (int e = 0; e < n; e += 2) word |= (uint32_t)codes[row * cb + g * 4 + (e >> 1)] << (4 * e);
-        const float sc = mx_scale(__ldg(scales + (kWhole ? unit >> 2 : row * nb + (g >> 2))));
-        float o[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = mx_code_value(word >> (4 * e)) * sc;
-        T* to = values + (kWhole ? unit * 8 : row * cols + g * 8);
-        if constexpr (kWhole && sizeof(T) == 2) {
-            uint4 q;
-            q.x = ptx::pack_bf16(o[0], o[1]); q.y = ptx::pack_bf16(o[2], o[3]); q.z = ptx::pack_bf16(o[4], o[5]); q.w = ptx::pack_bf16(o[6], o[7]);
-            __stcs(reinterpret_cast<uint4*>(to), q);
-        } else if constexpr (kWhole) {
-            __stcs(reinterpret_cast<float4*>(to), make_float4(o[0], o[1], o[2], o[3]));
-            __stcs(reinterpret_cast<float4*>(to) + 1, make_float4(o[4], o[5], o[6], o[7]));
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < n) to[e] = Elem<T>::from_float(o[e]);
-        }
+            for (int e = 0; e < n; e += 2) word |= (uint32_t)codes[row * cb + (int64_t)g * 4 + (e >> 1)] << (4 * e);
+        const float sc = mx_scale(__ldg(scales + (kRows == kMxWhole ? unit >> 2 : row * nb + (g >> 2))));
+        mx_write_values<T, kRows>(values + (kRows == kMxWhole ? unit * 8 : row * cols + (int64_t)g * 8), word, sc, n);
     }
 }
 

@@ -23,11 +23,12 @@ namespace fff {
 
 constexpr int kBalThreads = 1024;
 constexpr int kBalCols = 256;                 // columns (leaves) per tile
-constexpr int kBalMaxSlices = 296;            // row slices per tile when one tile has all columns: two CTAs per SM
+// Row slices per tile: a CTA per SM for one tile (the last CTA of a tile adds up its slices, and more of them cost more there than they
+// bring), two rounds of CTAs where the tiles are many.
+__host__ inline int balance_max_slices(int tiles) { return tiles <= 4 ? 148 / tiles : tiles < 296 ? 296 / tiles : 1; }
 
 struct BalanceScratch {
-    float* sums;            // [slices][L]
-    int32_t* counts;        // [slices][L]
+    float2* parts;          // [slices][L] sum of mix_j, tokens of leaf j (as int bits)
     int32_t* rows;          // [tiles][slices] tokens that count
     double* loss;           // [tiles] sum of counts_j * (sum of mix_j)
     int* done;              // [tiles] + [1], zero between calls
@@ -41,14 +42,13 @@ __device__ __forceinline__ bool token_counts(const int32_t* __restrict__ leaf_id
 // Grid (slices, tiles).  Every CTA adds up its rows of its columns and counts its rows' leaves among them; the last CTA of a tile
 // adds up the slices in their order, the last tile the tiles: one launch, and the same bits every time.
 // V: columns per thread (4; 1 for one or two leaves).  Rows are added in float32 (at most a few hundred each), slices in float64.
-// 65 536 tokens, 2048 leaves (537 MB): measured in the table of routing losses; rows of one tile are 1 KB apart reads of 1 KB.
 template <int V>
-__global__ void __launch_bounds__(kBalThreads, 2)
+__global__ void __launch_bounds__(kBalThreads, 1)
 k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask,
                float* __restrict__ loss, int32_t* __restrict__ counts, float* __restrict__ mean, int64_t B, int n_leaves,
                BalanceScratch ws)
 {
-    constexpr int U = 4;                                  // rows whose loads are in flight
+    constexpr int U = 8;                                  // rows whose loads are in flight
     __shared__ int s_hist[kBalCols];
     __shared__ float s_sum[kBalThreads * V], s_part[kBalThreads];
     __shared__ double s_loss[kBalThreads / 32];
@@ -117,8 +117,7 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
     if (tid < cols) {
         float sum = 0.0f;
         for (int k = 0; k < parts; ++k) sum += s_part[k * cols + i];
-        ws.sums[(int64_t)blockIdx.x * n_leaves + col0 + i] = sum;
-        ws.counts[(int64_t)blockIdx.x * n_leaves + col0 + i] = s_hist[i];
+        ws.parts[(int64_t)blockIdx.x * n_leaves + col0 + i] = make_float2(sum, __int_as_float(s_hist[i]));
     }
     if (tid == 0) ws.rows[blockIdx.y * slices + blockIdx.x] = s_rows;
     __threadfence();
@@ -137,10 +136,16 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
     const int down2 = kBalThreads / cols;
     double sum = 0.0;
     int cnt = 0;
-#pragma unroll 4
-    for (int s = r2; s < slices; s += down2) {
-        sum += (double)__ldcg(ws.sums + (int64_t)s * n_leaves + col0 + i);
-        cnt += __ldcg(ws.counts + (int64_t)s * n_leaves + col0 + i);
+    for (int s = r2; s < slices; s += 16 * down2) {
+        float2 part[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            part[k] = s + k * down2 < slices ? __ldcg(ws.parts + (int64_t)(s + k * down2) * n_leaves + col0 + i) : make_float2(0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            sum += (double)part[k].x;
+            cnt += __float_as_int(part[k].y);
+        }
     }
     __shared__ double s_col[kBalThreads];
     __shared__ int s_cnt[kBalThreads];
@@ -298,8 +303,8 @@ __device__ __forceinline__ float node_gradient(float ml, float sl, float mr, flo
 }
 
 // kUp: dmixture given; kBal: counts and dloss given (slope table for more than kRouteMaxStagedLeaves leaves).
-// A CTA takes route_rows rows at a time; its warps reduce chunks of 128 leaves (four levels in a lane's registers and across
-// neighbouring lanes, seven in all), then the levels above; the rows' gradients are collected in shared memory and leave as
+// A CTA takes route_rows rows at a time; its warps reduce chunks of 128 leaves (two levels in a lane's registers, up to five across
+// the lanes), then the levels above; the rows' gradients are collected in shared memory and leave as
 // aligned 16-byte vectors (a row has 2^d - 1 of them, so rows start anywhere).  Rows with a zero mask give zeros.
 template <bool kUp, bool kBal>
 __global__ void __launch_bounds__(kRouteThreads, kRoutePerSm)
@@ -326,21 +331,21 @@ k_routing_backward(const float* __restrict__ mix, const float* __restrict__ dmix
     const int64_t groups = (B + R - 1) / R;
     for (int64_t grp = blockIdx.x; grp < groups; grp += gridDim.x) {
         const int64_t row0 = grp * R;
-        const int rows = (int)min((int64_t)R, B - row0);
-        const int64_t elems = (int64_t)rows * L;
-        const int units = (int)((elems + kRouteChunk - 1) / kRouteChunk);
+        const int rows = (int)min((int64_t)R, B - row0), elems = rows * L;
+        const int units = (elems + kRouteChunk - 1) / kRouteChunk;
         const float* gm = mix + row0 * L;
         const float* gd = kUp ? dmix + row0 * L : nullptr;
         float* out = staged ? s_out : dz + row0 * N;
-        constexpr int U = 4;                                             // chunks whose loads are in flight
+        constexpr int U = 4;                                             // chunks that a warp reduces together
         for (int u0 = warp; u0 < units; u0 += U * kRouteWarps) {
             float m4[U][4], g4[U][4];
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int64_t e = (int64_t)(u0 + i * kRouteWarps) * kRouteChunk + lane * 4;
+                const int e = (u0 + i * kRouteWarps) * kRouteChunk + lane * 4;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) { m4[i][k] = 0.0f; g4[i][k] = 0.0f; }
                 if (e >= elems) continue;
+                // (L = 2: a lane's four weights are two rows, and the last lane may have one)
                 if (depth >= 2 || e + 4 <= elems) {
                     const float4 q = __ldcs(reinterpret_cast<const float4*>(gm + e));
                     m4[i][0] = q.x; m4[i][1] = q.y; m4[i][2] = q.z; m4[i][3] = q.w;
@@ -354,6 +359,11 @@ k_routing_backward(const float* __restrict__ mix, const float* __restrict__ dmix
                         if constexpr (kUp) g4[i][k] = gd[e + k];
                     }
                 }
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int e = (u0 + i * kRouteWarps) * kRouteChunk + lane * 4;
+                if (e >= elems) continue;
                 // the lane's row, or (L = 2) its two rows
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
@@ -361,10 +371,15 @@ k_routing_backward(const float* __restrict__ mix, const float* __restrict__ dmix
                     const int64_t b = row0 + ((e + 2 * half) >> depth);
                     const int k0 = 2 * half, k1 = depth >= 2 ? 4 : k0 + 2;
                     if (kBal && (!leaf_idx || (unsigned)__ldg(leaf_idx + b) < (unsigned)L)) {
-                        const float* table = (staged ? s_slope : slope_table) + (depth >= 2 ? (int)(e & (L - 1)) : -k0);
+                        const float* table = (staged ? s_slope : slope_table) + (depth >= 2 ? e & (L - 1) : -k0);
+                        if (depth >= 2) {
+                            const float4 q = *reinterpret_cast<const float4*>(table);
+                            g4[i][0] += q.x; g4[i][1] += q.y; g4[i][2] += q.z; g4[i][3] += q.w;
+                        } else {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (k >= k0 && k < k1) g4[i][k] += table[k];
+                            for (int k = 0; k < 4; ++k)
+                                if (k >= k0 && k < k1) g4[i][k] += table[k];
+                        }
                     }
                     if (mask && __ldg(mask + b) == 0) {
 #pragma unroll
@@ -373,45 +388,66 @@ k_routing_backward(const float* __restrict__ mix, const float* __restrict__ dmix
                     }
                 }
             }
+            // two levels in the lane's registers
+            float m[U], t[U];                                            // sums over the lane's four leaves
 #pragma unroll
             for (int i = 0; i < U; ++i) {
-                const int unit = u0 + i * kRouteWarps;
-                if (unit >= units) break;
-                const int64_t e = (int64_t)unit * kRouteChunk + lane * 4;
-                const bool in = e < elems;
-                const int row = (int)(e >> depth), j = (int)(e & (L - 1));
-                float* o = out + (int64_t)row * N;
-                const float (&m)[4] = m4[i];
+                const int e = (u0 + i * kRouteWarps) * kRouteChunk + lane * 4, row = e >> depth, j = e & (L - 1);
                 float ma, sa, mb, sb;
-                const float g0 = node_gradient(m[0], m[0] * g4[i][0], m[1], m[1] * g4[i][1], ma, sa);
-                const float g1 = node_gradient(m[2], m[2] * g4[i][2], m[3], m[3] * g4[i][3], mb, sb);
+                const float (&w)[4] = m4[i];
+                const float g0 = node_gradient(w[0], w[0] * g4[i][0], w[1], w[1] * g4[i][1], ma, sa);
+                const float g1 = node_gradient(w[2], w[2] * g4[i][2], w[3], w[3] * g4[i][3], mb, sb);
+                const float g2 = node_gradient(ma, sa, mb, sb, m[i], t[i]);
+                if (e >= elems) continue;
                 if (depth == 1) {
-                    if (in) {
-                        out[row] = g0;
-                        if (e + 2 < elems) out[row + 1] = g1;
-                    }
-                    continue;
+                    out[row] = g0;
+                    if (e + 2 < elems) out[row + 1] = g1;
+                } else {
+                    float* o = out + row * N;
+                    const int last = (1 << (depth - 1)) - 1 + (j >> 1);  // first of two nodes above the leaves
+                    o[last] = g0;
+                    o[last + 1] = g1;
+                    o[(1 << (depth - 2)) - 1 + (j >> 2)] = g2;
                 }
-                const int last = (1 << (depth - 1)) - 1;                 // first node of the level above the leaves
-                if (in) {
-                    o[last + (j >> 1)] = g0;
-                    o[last + (j >> 1) + 1] = g1;
-                }
-                float mm, ss;
-                const float g2 = node_gradient(ma, sa, mb, sb, mm, ss);
-                if (in) o[(1 << (depth - 2)) - 1 + (j >> 2)] = g2;
-                // one more level per step: 2^k lanes share a node of level depth - 2 - k
+            }
+            // Up to five more across the lanes.  The chunks are shared out on the way: after the first step a lane goes on with two of
+            // the four, after the second with one, so that a level costs what its nodes do (every lane going on with all four: 20
+            // nodes and 40 shuffles instead of 6 and 12).
+            auto store = [&](int i, int k, float g) {                    // node 2^(2+k) leaves wide of chunk i
+                const int unit = u0 + i * kRouteWarps, e = unit * kRouteChunk + (lane & ~((1 << k) - 1)) * 4;
+                if (e < elems) out[(e >> depth) * N + (1 << (depth - 2 - k)) - 1 + ((e & (L - 1)) >> (2 + k))] = g;
+            };
+            const bool r0 = lane & 1, r1 = lane & 2;
+            float mm, ss;
+            if (depth >= 3) {
+                float m2[2], t2[2];
 #pragma unroll
-                for (int k = 1; k <= 5; ++k) {
-                    if (k > depth - 2) break;
-                    const float mo = __shfl_xor_sync(kFullMask, mm, 1 << (k - 1)), so = __shfl_xor_sync(kFullMask, ss, 1 << (k - 1));
-                    const bool right = (lane >> (k - 1)) & 1;
-                    const float g = node_gradient(right ? mo : mm, right ? so : ss, right ? mm : mo, right ? ss : so, mm, ss);
-                    if (in && (lane & ((1 << k) - 1)) == 0) o[(1 << (depth - 2 - k)) - 1 + (j >> (2 + k))] = g;
+                for (int i = 0; i < 2; ++i) {
+                    // chunk i stays with even lanes, chunk 2 + i with odd ones
+                    const float mo = __shfl_xor_sync(kFullMask, r0 ? m[i] : m[2 + i], 1), to = __shfl_xor_sync(kFullMask, r0 ? t[i] : t[2 + i], 1);
+                    const float mk = r0 ? m[2 + i] : m[i], tk = r0 ? t[2 + i] : t[i];
+                    const float g = node_gradient(r0 ? mo : mk, r0 ? to : tk, r0 ? mk : mo, r0 ? tk : to, m2[i], t2[i]);
+                    store(r0 ? 2 + i : i, 1, g);
                 }
-                if (chunks > 1 && lane == 0) {
-                    s_top[unit] = mm;                                    // unit = row * chunks + chunk
-                    s_top[R * chunks + unit] = ss;
+                if (depth >= 4) {
+                    const float mo = __shfl_xor_sync(kFullMask, r1 ? m2[0] : m2[1], 2), to = __shfl_xor_sync(kFullMask, r1 ? t2[0] : t2[1], 2);
+                    const float mk = r1 ? m2[1] : m2[0], tk = r1 ? t2[1] : t2[0];
+                    const int mine = (r0 ? 2 : 0) + (r1 ? 1 : 0);
+                    float g = node_gradient(r1 ? mo : mk, r1 ? to : tk, r1 ? mk : mo, r1 ? tk : to, mm, ss);
+                    store(mine, 2, g);
+#pragma unroll
+                    for (int k = 3; k <= 5; ++k) {
+                        if (k > depth - 2) break;
+                        const float mx = __shfl_xor_sync(kFullMask, mm, 1 << (k - 1)), sx = __shfl_xor_sync(kFullMask, ss, 1 << (k - 1));
+                        const bool right = (lane >> (k - 1)) & 1;
+                        g = node_gradient(right ? mx : mm, right ? sx : ss, right ? mm : mx, right ? ss : sx, mm, ss);
+                        if (((lane >> 2) & ((1 << (k - 2)) - 1)) == 0) store(mine, k, g);
+                    }
+                    const int unit = u0 + mine * kRouteWarps;
+                    if (chunks > 1 && lane < 4 && unit < units) {
+                        s_top[unit] = mm;                                // unit = row * chunks + chunk
+                        s_top[R * chunks + unit] = ss;
+                    }
                 }
             }
         }

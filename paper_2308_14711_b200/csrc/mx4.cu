@@ -31,15 +31,16 @@ unsigned spread(int64_t units, int threads, int sm_count, int per_sm) {
 template <typename T>
 cudaError_t quantize(const LaunchOn& on, const T* src, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales, T* values) {
     const unsigned grid = spread((rows * mx_scales(cols) * 4 + 1) / 2, 256, on.sm_count, 8);
-    return launch_on(on, cols % kMxBlock == 0 ? k_quantize_mx4<T, true> : k_quantize_mx4<T, false>, grid, 1, 256, 0, src, codes, scales, values,
-                     rows, cols);
+    const auto kern = cols % kMxBlock == 0 ? k_quantize_mx4<T, kMxWhole> : cols % 8 == 0 ? k_quantize_mx4<T, kMxGroups> : k_quantize_mx4<T, kMxAny>;
+    return launch_on(on, kern, grid, 1, 256, 0, src, codes, scales, values, rows, cols);
 }
 
 template <typename T>
 cudaError_t dequantize(const LaunchOn& on, const uint8_t* codes, const uint8_t* scales, T* values, int64_t rows, int64_t cols) {
     const unsigned grid = spread(rows * mx_scales(cols) * 4, 256, on.sm_count, 16);
-    return launch_on(on, cols % kMxBlock == 0 ? k_dequantize_mx4<T, true> : k_dequantize_mx4<T, false>, grid, 1, 256, 0, codes, scales, values,
-                     rows, cols);
+    const auto kern =
+        cols % kMxBlock == 0 ? k_dequantize_mx4<T, kMxWhole> : cols % 8 == 0 ? k_dequantize_mx4<T, kMxGroups> : k_dequantize_mx4<T, kMxAny>;
+    return launch_on(on, kern, grid, 1, 256, 0, codes, scales, values, rows, cols);
 }
 
 template <int MT, bool kWide, bool kBig>

@@ -13,7 +13,6 @@ namespace {
 constexpr int kMaxDevices = 64;
 
 int balance_tiles(int64_t n_leaves) { return (int)std::max<int64_t>(1, n_leaves / kBalCols); }
-int balance_max_slices(int64_t n_leaves) { return std::max(1, kBalMaxSlices / balance_tiles(n_leaves)); }
 
 // Slices so that every thread of a CTA has a few rows to add up; one where the whole batch is little more than that.
 int slices_for(int64_t B, int64_t n_leaves, int threads, int rows_each, int most) {
@@ -22,28 +21,29 @@ int slices_for(int64_t B, int64_t n_leaves, int threads, int rows_each, int most
 }
 
 BalanceScratch layout(void* scratch, int64_t n_leaves) {
-    const size_t S = balance_max_slices(n_leaves), T = balance_tiles(n_leaves);
+    const size_t S = balance_max_slices(balance_tiles(n_leaves)), T = balance_tiles(n_leaves);
     BalanceScratch ws;
     ws.loss = static_cast<double*>(scratch);
-    ws.sums = reinterpret_cast<float*>(ws.loss + T);
-    ws.counts = reinterpret_cast<int32_t*>(ws.sums + S * n_leaves);
-    ws.rows = ws.counts + S * n_leaves;
+    ws.parts = reinterpret_cast<float2*>(ws.loss + T);
+    ws.rows = reinterpret_cast<int32_t*>(ws.parts + S * n_leaves);
     ws.done = ws.rows + S * T;
     return ws;
 }
 
 }  // namespace
 
-float* balance_scratch_slope(void* scratch, int64_t n_leaves) { return layout(scratch, n_leaves).sums; }
+float* balance_scratch_slope(void* scratch, int64_t n_leaves) {
+    return reinterpret_cast<float*>(layout(scratch, n_leaves).parts);
+}
 
 size_t balance_scratch_bytes(int64_t n_leaves) {
-    const size_t S = balance_max_slices(n_leaves), T = balance_tiles(n_leaves);
+    const size_t S = balance_max_slices(balance_tiles(n_leaves)), T = balance_tiles(n_leaves);
     return 8 * T + 8 * S * n_leaves + 4 * S * T + 4 * (T + 1);
 }
 
 cudaError_t balance_loss(const LaunchOn& on, const float* mixture, const int32_t* leaf_idx, const uint8_t* mask, float* loss,
                          int32_t* counts, float* mean, int64_t B, int64_t n_leaves, void* scratch) {
-    const int S = slices_for(B, n_leaves, kBalThreads, 4, balance_max_slices(n_leaves));
+    const int S = slices_for(B, n_leaves, kBalThreads, 4, balance_max_slices(balance_tiles(n_leaves)));
     const unsigned T = (unsigned)balance_tiles(n_leaves);
     return launch_on(on, n_leaves >= 4 ? k_balance_loss<4> : k_balance_loss<1>, (unsigned)S, T, kBalThreads, 0, mixture, leaf_idx, mask, loss,
                      counts, mean, B, (int)n_leaves, layout(scratch, n_leaves));
