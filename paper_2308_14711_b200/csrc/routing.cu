@@ -70,7 +70,7 @@ cudaError_t routing_backward(const LaunchOn& on, const float* mixture, const flo
         ++*launches;
     }
     const auto kern = up ? (bal ? k_routing_backward<true, true> : k_routing_backward<true, false>) : k_routing_backward<false, true>;
-    const size_t smem = route_smem(L, bal);
+    const size_t smem = RouteSmem{L, bal}.bytes();
     const int which = up ? (bal ? 0 : 1) : 2;
     if (smem > 48 * 1024) {
         static std::mutex mu;
@@ -84,7 +84,9 @@ cudaError_t routing_backward(const LaunchOn& on, const float* mixture, const flo
     }
     const int64_t groups = (B + route_rows(L) - 1) / route_rows(L);
     const int per_sm = (int)std::max<size_t>(1, std::min<size_t>(kRoutePerSm, (size_t)(227 * 1024) / (smem + 1024)));
-    const unsigned grid = (unsigned)std::min<int64_t>(groups, (int64_t)on.sm_count * per_sm);
+    const int64_t ctas = route_by_warps(L) ? (groups + kRouteWarps - 1) / kRouteWarps : groups;
+    // (a batch that would not give every SM a CTA: a warp of work each)
+    const unsigned grid = (unsigned)std::min<int64_t>(ctas < on.sm_count ? groups : ctas, (int64_t)on.sm_count * per_sm);
     const cudaError_t e = launch_on(on, kern, grid, 1, kRouteThreads, smem, mixture, dmixture, leaf_idx, mask, counts, dloss,
                                     (const float*)slope, dlogits, B, depth);
     if (e == cudaSuccess) ++*launches;
