@@ -102,8 +102,9 @@ _call = None
 
 
 def torch_call():
-    """The CPython module behind FFFLayer.forward_infer (csrc/torch_call.cpp), told where fff_forward_infer is (once).  None where it
-    has not been built for this interpreter and torch: the call then goes through ctypes, for about 5 us more of host time."""
+    """The CPython module behind FFFLayer.forward_infer, the routing losses and quantize_mx4 (csrc/torch_call.cpp), told where the
+    library's functions are (once).  None where it has not been built for this interpreter and torch: the calls then go through ctypes,
+    for 5 to 10 us more of host time."""
     global _call
     if _call is None:
         import importlib.util
@@ -115,7 +116,9 @@ def torch_call():
         spec = importlib.util.spec_from_file_location("torch_call", path)
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)
-        mod.set_address(C.cast(lib().fff_forward_infer, C.c_void_p).value)
+        L = lib()
+        mod.set_addresses(*[C.cast(f, C.c_void_p).value for f in (L.fff_forward_infer, L.fff_balance_loss, L.fff_balance_loss_backward,
+                                                                  L.fff_routing_backward, L.fff_quantize_mx4)])
         _call = mod
     return _call
 
@@ -262,6 +265,11 @@ def quantize_mx4(w, want_values: bool = False, stream=None):
     (codes, scales, values) with the numbers that the codes stand for in w's type.  codes uint8 [..., (cols + 1) // 2], two per byte,
     scales uint8 [..., (cols + 31) // 32]."""
     torch = _torch()
+    call = torch_call()
+    got = None if call is None else call.quantize_mx4(w, want_values, None if stream is None else stream.cuda_stream)
+    if got is not None:
+        _check(got[0], "fff_quantize_mx4")
+        return got[1:] if want_values else got[1:3]
     if w.dim() < 1:
         raise ValueError("w: expected rows")
     cols, lead = w.shape[-1], tuple(w.shape[:-1])
@@ -324,7 +332,7 @@ class FFFLayer:
 
     def _bind_forward(self) -> None:
         self._bf16 = self.tdtype == _torch().bfloat16
-        call = torch_call()
+        self._call = call = torch_call()
         self._forward = call.forward if call is not None else lambda *args: None
 
     @classmethod
@@ -420,6 +428,11 @@ class FFFLayer:
     def balance_loss(self, mixture, leaf_idx, token_mask=None, stream=None):
         """The balance loss of a batch (mixture [B, 2^d] float32 of forward_train, leaf_idx [B] int32, token_mask [B] bool or uint8, False or
         0 for tokens to leave out): returns (loss float32, counts int32 [2^d], mean mixture weights float32 [2^d])."""
+        if self._call is not None:
+            got = self._call.balance_loss(self._h, self.n_leaves, mixture, leaf_idx, token_mask, None if stream is None else stream.cuda_stream)
+            if got is not None:
+                _check(got[0], "fff_balance_loss")
+                return got[1:]
         torch = _torch()
         B, dev = mixture.shape[0], mixture.device
         mp, lp = _ptr(mixture, torch.float32, (B, self.n_leaves), "mixture"), _ptr(leaf_idx, torch.int32, (B,), "leaf_idx")
@@ -432,6 +445,12 @@ class FFFLayer:
 
     def balance_loss_backward(self, leaf_idx, counts, dloss, token_mask=None, stream=None):
         """Gradient of the balance loss with respect to the mixture weights, float32 [B, 2^d]; dloss: one float32 on the device."""
+        if self._call is not None:
+            got = self._call.balance_loss_backward(self._h, self.n_leaves, leaf_idx, counts, dloss, token_mask,
+                                                   None if stream is None else stream.cuda_stream)
+            if got is not None:
+                _check(got[0], "fff_balance_loss_backward")
+                return got[1]
         torch = _torch()
         B = leaf_idx.shape[0]
         lp, cp = _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"), _ptr(counts, torch.int32, (self.n_leaves,), "counts")
@@ -444,6 +463,12 @@ class FFFLayer:
     def routing_backward(self, mixture, dmixture=None, leaf_idx=None, counts=None, dloss=None, token_mask=None, stream=None):
         """Gradient with respect to the node logits, float32 [B, 2^d - 1], of a loss with gradient dmixture [B, 2^d] (may be None) plus, where
         counts and dloss are given, of the balance loss."""
+        if self._call is not None:
+            got = self._call.routing_backward(self._h, self.n_leaves, mixture, dmixture, leaf_idx, counts, dloss, token_mask,
+                                              None if stream is None else stream.cuda_stream)
+            if got is not None:
+                _check(got[0], "fff_routing_backward")
+                return got[1]
         torch = _torch()
         B = mixture.shape[0]
         f32 = torch.float32

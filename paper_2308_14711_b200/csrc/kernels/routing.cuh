@@ -21,29 +21,35 @@ namespace fff {
 
 // ---- balance loss ----------------------------------------------------------------------------------
 
-constexpr int kBalThreads = 1024;
-constexpr int kBalCols = 256;                 // columns (leaves) per tile
-// Row slices per tile: a CTA per SM for one tile (the last CTA of a tile adds up its slices, and more of them cost more there than they
-// bring), two rounds of CTAs where the tiles are many.
-__host__ inline int balance_max_slices(int tiles) { return tiles <= 4 ? 148 / tiles : tiles < 296 ? 296 / tiles : 1; }
+constexpr int kBalThreads = 512;
+constexpr int kBalCols = 512;                 // columns (leaves) per tile
+constexpr int kBalGroup = 16;                 // slices that one CTA adds up
+// Row slices per tile: two CTAs per SM.
+__host__ inline int balance_max_slices(int tiles) { return tiles < 296 ? 296 / tiles : 1; }
+__host__ __device__ inline int balance_groups(int slices) { return (slices + kBalGroup - 1) / kBalGroup; }
 
 struct BalanceScratch {
     float2* parts;          // [slices][L] sum of mix_j, tokens of leaf j (as int bits)
+    double* group_sums;     // [groups][L] the same of a group of slices
+    int32_t* group_counts;  // [groups][L]
     int32_t* rows;          // [tiles][slices] tokens that count
+    int32_t* group_rows;    // [tiles][groups]
     double* loss;           // [tiles] sum of counts_j * (sum of mix_j)
-    int* done;              // [tiles] + [1], zero between calls
+    int* done;              // [tiles][groups + 1] + [1], zero between calls
 };
 
-__device__ __forceinline__ bool token_counts(const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask, int64_t b, int n_leaves, int& leaf) {
-    leaf = __ldg(leaf_idx + b);
-    return (unsigned)leaf < (unsigned)n_leaves && (!mask || __ldg(mask + b) != 0);
+// Leaf of a token, -1 if it does not count.  (Both loads are sent for at once.)
+__device__ __forceinline__ int counted_leaf(const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask, int64_t b, int n_leaves) {
+    const int leaf = leaf_idx ? __ldg(leaf_idx + b) : 0;
+    const int kept = mask ? __ldg(mask + b) : 1;
+    return (unsigned)leaf < (unsigned)n_leaves && kept ? leaf : -1;
 }
 
 // Grid (slices, tiles).  Every CTA adds up its rows of its columns and counts its rows' leaves among them; the last CTA of a tile
 // adds up the slices in their order, the last tile the tiles: one launch, and the same bits every time.
 // V: columns per thread (4; 1 for one or two leaves).  Rows are added in float32 (at most a few hundred each), slices in float64.
 template <int V>
-__global__ void __launch_bounds__(kBalThreads, 1)
+__global__ void __launch_bounds__(kBalThreads, 2)
 k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask,
                float* __restrict__ loss, int32_t* __restrict__ counts, float* __restrict__ mean, int64_t B, int n_leaves,
                BalanceScratch ws)
@@ -72,9 +78,11 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
     const float* base = mix + col0 + c * V;
     for (int64_t b = b0 + r; b < b1; b += (int64_t)U * down) {
         float m[U][V];
+        int leaf[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = b + (int64_t)u * down;
+            leaf[u] = row < b1 ? counted_leaf(leaf_idx, mask, row, n_leaves) : -1;
 #pragma unroll
             for (int v = 0; v < V; ++v) m[u][v] = 0.0f;
             if (row >= b1) continue;
@@ -87,15 +95,12 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t row = b + (int64_t)u * down;
-            int leaf;
             // (rows that do not count are left out, not multiplied by zero: they may hold anything)
-            if (row >= b1 || !token_counts(leaf_idx, mask, row, n_leaves, leaf)) continue;
 #pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] += m[u][v];
-            if (c == 0) {
+            for (int v = 0; v < V; ++v) acc[v] += leaf[u] >= 0 ? m[u][v] : 0.0f;
+            if (c == 0 && leaf[u] >= 0) {
                 ++mine;
-                if ((unsigned)(leaf - col0) < (unsigned)cols) atomicAdd(&s_hist[leaf - col0], 1);
+                if ((unsigned)(leaf[u] - col0) < (unsigned)cols) atomicAdd(&s_hist[leaf[u] - col0], 1);
             }
         }
     }
@@ -119,47 +124,72 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
         for (int k = 0; k < parts; ++k) mine_sum += s_part[k * cols + i];
     double sum = (double)mine_sum;
     int cnt = tid < cols ? s_hist[i] : 0;
-    if (slices > 1) {
-        if (tid < cols) ws.parts[(int64_t)blockIdx.x * n_leaves + col0 + i] = make_float2(mine_sum, __int_as_float(cnt));
-        if (tid == 0) ws.rows[blockIdx.y * slices + blockIdx.x] = s_rows;
+    // Slices are added up by the last CTA of their group, groups by the last of the tile (148 slices by one CTA alone: 8 us).
+    const int groups = balance_groups(slices), group = blockIdx.x / kBalGroup, first = group * kBalGroup;
+    const int members = min(kBalGroup, slices - first);
+    int* done = ws.done + blockIdx.y * (groups + 1);
+    // whether this CTA is the last of `of` to have written what it has, which it then sees
+    auto last_of = [&](int* counter, int of) {
         __threadfence();
         __syncthreads();
-        if (tid == 0) s_last = atomicAdd(ws.done + blockIdx.y, 1) == slices - 1;
-        __syncthreads();
-        if (!s_last) return;
-        __threadfence();
-
-        // ---- the tile's last CTA: several threads per column, then one
-        if (tid == 0) { s_rows = 0; ws.done[blockIdx.y] = 0; }
-        __syncthreads();
-        int rows = 0;
-        for (int s = tid; s < slices; s += kBalThreads) rows += __ldcg(ws.rows + blockIdx.y * slices + s);
-        if (rows) atomicAdd(&s_rows, rows);
-        const int down2 = kBalThreads / cols;
-        sum = 0.0;
-        cnt = 0;
-        for (int s = r2; s < slices; s += 16 * down2) {
-            float2 part[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k)
-                part[k] = s + k * down2 < slices ? __ldcg(ws.parts + (int64_t)(s + k * down2) * n_leaves + col0 + i) : make_float2(0.0f, 0.0f);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                sum += (double)part[k].x;
-                cnt += __float_as_int(part[k].y);
-            }
+        if (tid == 0) {
+            s_last = atomicAdd(counter, 1) == of - 1;
+            if (s_last) { *counter = 0; s_rows = 0; }
         }
-        __shared__ double s_col[kBalThreads];
-        __shared__ int s_cnt[kBalThreads];
+        __syncthreads();
+        if (s_last) __threadfence();
+        return s_last;
+    };
+    __shared__ double s_col[kBalThreads];
+    __shared__ int s_cnt[kBalThreads];
+    const int each = kBalThreads / cols;                  // threads per column
+    // what the threads of a column have, in the column's first
+    auto add_columns = [&](int of) {
         s_col[tid] = sum;
         s_cnt[tid] = cnt;
         __syncthreads();
         if (tid < cols)
-            for (int k = 1; k < min(down2, slices); ++k) {
+            for (int k = 1; k < min(each, of); ++k) {
                 sum += s_col[k * cols + i];
                 cnt += s_cnt[k * cols + i];
             }
+    };
+    if (slices > 1) {
+        if (tid < cols) ws.parts[(int64_t)blockIdx.x * n_leaves + col0 + i] = make_float2(mine_sum, __int_as_float(cnt));
+        if (tid == 0) ws.rows[blockIdx.y * slices + blockIdx.x] = s_rows;
+        if (!last_of(done + group, members)) return;
+        if (tid < members) atomicAdd(&s_rows, __ldcg(ws.rows + blockIdx.y * slices + first + tid));
+        float2 part[kBalGroup];
+#pragma unroll
+        for (int k = 0; k < kBalGroup; ++k)
+            part[k] = r2 + k * each < members ? __ldcg(ws.parts + (int64_t)(first + r2 + k * each) * n_leaves + col0 + i) : make_float2(0.0f, 0.0f);
+        sum = 0.0;
+        cnt = 0;
+#pragma unroll
+        for (int k = 0; k < kBalGroup; ++k) {
+            sum += (double)part[k].x;
+            cnt += __float_as_int(part[k].y);
+        }
+        add_columns(members);
+        if (groups > 1) {
+            if (tid < cols) {
+                ws.group_sums[(int64_t)group * n_leaves + col0 + i] = sum;
+                ws.group_counts[(int64_t)group * n_leaves + col0 + i] = cnt;
+            }
+            if (tid == 0) ws.group_rows[blockIdx.y * groups + group] = s_rows;
+            if (!last_of(done + groups, groups)) return;
+            if (tid < groups) atomicAdd(&s_rows, __ldcg(ws.group_rows + blockIdx.y * groups + tid));
+            sum = 0.0;
+            cnt = 0;
+#pragma unroll 10
+            for (int k = r2; k < groups; k += each) {
+                sum += __ldcg(ws.group_sums + (int64_t)k * n_leaves + col0 + i);
+                cnt += __ldcg(ws.group_counts + (int64_t)k * n_leaves + col0 + i);
+            }
+            add_columns(groups);
+        }
     }
+    __syncthreads();
     const double n = (double)s_rows, inv = n > 0.0 ? 1.0 / n : 0.0;
     double part = 0.0;
     if (tid < cols) {
@@ -167,6 +197,7 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
         if (mean) mean[col0 + i] = (float)(n > 0.0 ? sum * inv : 0.0);
         part = cnt == 0 ? 0.0 : (double)cnt * sum;        // (not 0 times a sum that overflowed)
     }
+    int* all_done = ws.done + tiles * (groups + 1);
     // (the columns' warps, which come first)
     const int col_warps = (cols + 31) / 32;
     if ((tid >> 5) < col_warps) {
@@ -183,7 +214,7 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
         } else {
             ws.loss[blockIdx.y] = t;
             __threadfence();
-            s_last = atomicAdd(ws.done + tiles, 1) == tiles - 1;
+            s_last = atomicAdd(all_done, 1) == tiles - 1;
         }
     }
     if (tiles == 1) return;
@@ -200,7 +231,7 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
         double t = 0.0;
         for (int w = 0; w < min(kBalThreads / 32, (tiles + 31) / 32); ++w) t += s_loss[w];
         if (loss) loss[0] = (float)((double)n_leaves * t * inv * inv);
-        ws.done[tiles] = 0;
+        *all_done = 0;
     }
 }
 
@@ -250,8 +281,7 @@ k_balance_loss_backward(const int32_t* __restrict__ leaf_idx, const uint8_t* __r
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = b + (int64_t)u * down;
-            int leaf;
-            in[u] = row < b1 && (leaf_idx ? token_counts(leaf_idx, mask, row, n_leaves, leaf) : (!mask || __ldg(mask + row) != 0));
+            in[u] = row < b1 && counted_leaf(leaf_idx, mask, row, n_leaves) >= 0;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -333,12 +363,17 @@ __device__ __forceinline__ void route_chunk(const float* __restrict__ gm, const 
     constexpr int U = 4;
     const int L = 1 << depth, N = L - 1;
     float m4[U][4], g4[U][4];
+    int leaf[U], kept[U];                                  // of the lane's row (depth >= 2)
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int e = base + i * 128 + lane * 4;
 #pragma unroll
         for (int k = 0; k < 4; ++k) { m4[i][k] = 0.0f; g4[i][k] = 0.0f; }
+        leaf[i] = 0;
+        kept[i] = 1;
         if (e >= elems) continue;
+        if (kBal && leaf_idx) leaf[i] = __ldg(leaf_idx + row0 + (e >> depth));
+        if (mask) kept[i] = __ldg(mask + row0 + (e >> depth));
         // (L = 2: a lane's four weights are two rows, and the last lane may have one)
         if (depth >= 2 || e + 4 <= elems) {
             const float4 q = __ldcs(reinterpret_cast<const float4*>(gm + e));
@@ -359,26 +394,26 @@ __device__ __forceinline__ void route_chunk(const float* __restrict__ gm, const 
         for (int i = 0; i < U; ++i) {
             const int e = base + i * 128 + lane * 4;
             if (e >= elems) continue;
-            // the lane's row, or (L = 2) its two rows
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (half == 1 && (depth >= 2 || e + 2 >= elems)) break;
-                const int64_t b = row0 + ((e + 2 * half) >> depth);
-                const int k0 = 2 * half, k1 = depth >= 2 ? 4 : k0 + 2;
-                if (kBal && (!leaf_idx || (unsigned)__ldg(leaf_idx + b) < (unsigned)L)) {
-                    if (depth >= 2) {
-                        const float4 q = *reinterpret_cast<const float4*>(slopes + (e & (L - 1)));
-                        g4[i][0] += q.x; g4[i][1] += q.y; g4[i][2] += q.z; g4[i][3] += q.w;
-                    } else {
-                        g4[i][k0] += slopes[0];
-                        g4[i][k0 + 1] += slopes[1];
-                    }
+            if (depth >= 2) {
+                if (kBal && (unsigned)leaf[i] < (unsigned)L) {
+                    const float4 q = *reinterpret_cast<const float4*>(slopes + (e & (L - 1)));
+                    g4[i][0] += q.x; g4[i][1] += q.y; g4[i][2] += q.z; g4[i][3] += q.w;
                 }
-                if (mask && __ldg(mask + b) == 0) {
+                if (!kept[i]) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (k >= k0 && k < k1) m4[i][k] = g4[i][k] = 0.0f;
+                    for (int k = 0; k < 4; ++k) m4[i][k] = g4[i][k] = 0.0f;
                 }
+                continue;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {               // (L = 2: two rows)
+                if (e + k >= elems) break;
+                const int64_t b = row0 + ((e + k) >> 1);
+                if (kBal && (!leaf_idx || (unsigned)__ldg(leaf_idx + b) < 2u)) {
+                    g4[i][k] += slopes[0];
+                    g4[i][k + 1] += slopes[1];
+                }
+                if (mask && __ldg(mask + b) == 0) m4[i][k] = m4[i][k + 1] = g4[i][k] = g4[i][k + 1] = 0.0f;
             }
         }
     }

@@ -21,12 +21,15 @@ int slices_for(int64_t B, int64_t n_leaves, int threads, int rows_each, int most
 }
 
 BalanceScratch layout(void* scratch, int64_t n_leaves) {
-    const size_t S = balance_max_slices(balance_tiles(n_leaves)), T = balance_tiles(n_leaves);
+    const size_t T = balance_tiles(n_leaves), S = balance_max_slices((int)T), G = balance_groups((int)S);
     BalanceScratch ws;
     ws.loss = static_cast<double*>(scratch);
-    ws.parts = reinterpret_cast<float2*>(ws.loss + T);
-    ws.rows = reinterpret_cast<int32_t*>(ws.parts + S * n_leaves);
-    ws.done = ws.rows + S * T;
+    ws.group_sums = ws.loss + ((T + 1) & ~(size_t)1);      // (the rest starts on a 16-byte boundary)
+    ws.parts = reinterpret_cast<float2*>(ws.group_sums + ((G * n_leaves + 1) & ~(size_t)1));
+    ws.group_counts = reinterpret_cast<int32_t*>(ws.parts + S * n_leaves);
+    ws.rows = ws.group_counts + G * n_leaves;
+    ws.group_rows = ws.rows + S * T;
+    ws.done = ws.group_rows + G * T;
     return ws;
 }
 
@@ -37,13 +40,14 @@ float* balance_scratch_slope(void* scratch, int64_t n_leaves) {
 }
 
 size_t balance_scratch_bytes(int64_t n_leaves) {
-    const size_t S = balance_max_slices(balance_tiles(n_leaves)), T = balance_tiles(n_leaves);
-    return 8 * T + 8 * S * n_leaves + 4 * S * T + 4 * (T + 1);
+    const size_t T = balance_tiles(n_leaves), S = balance_max_slices((int)T), G = balance_groups((int)S);
+    return 8 * (T + 1) + 8 * (G * n_leaves + 1) + 8 * S * n_leaves + 4 * (G * n_leaves + S * T + G * T + T * (G + 1) + 1);
 }
 
 cudaError_t balance_loss(const LaunchOn& on, const float* mixture, const int32_t* leaf_idx, const uint8_t* mask, float* loss,
                          int32_t* counts, float* mean, int64_t B, int64_t n_leaves, void* scratch) {
-    const int S = slices_for(B, n_leaves, kBalThreads, 4, balance_max_slices(balance_tiles(n_leaves)));
+    int S = slices_for(B, n_leaves, kBalThreads, 16, balance_max_slices(balance_tiles(n_leaves)));
+    if (S > kBalGroup && S <= 3 * kBalGroup) S = kBalGroup;      // (a second round of sums costs more than longer slices)
     const unsigned T = (unsigned)balance_tiles(n_leaves);
     return launch_on(on, n_leaves >= 4 ? k_balance_loss<4> : k_balance_loss<1>, (unsigned)S, T, kBalThreads, 0, mixture, leaf_idx, mask, loss,
                      counts, mean, B, (int)n_leaves, layout(scratch, n_leaves));

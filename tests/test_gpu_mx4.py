@@ -89,7 +89,8 @@ SPECIAL = [0.0, -0.0, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 5.5, 6.0, 7.0, 7.99
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 31), (3, 32), (5, 33), (7, 64), (2, 100), (129, 7), (64, 784), (1000, 96), (3, 4099), (0, 5), (4, 0)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 31), (3, 32), (5, 33), (7, 64), (2, 100), (129, 7), (64, 784), (1000, 96), (3, 4099), (70, 40), (90, 200),
+                                       (0, 5), (4, 0)])
 def test_conversion_is_the_definition(rows, cols, dtype):
     g = np.random.default_rng(rows * 10007 + cols)
     w = g.standard_normal((rows, cols)).astype(np.float32) * np.exp2(g.integers(-140, 120, size=(rows, 1)).astype(np.float32))
@@ -325,7 +326,10 @@ def test_layers_that_are_refused():
     assert e.value.status == 2
 
 
-def test_conversions_that_are_refused():
+@pytest.mark.parametrize("way", ["module", "ctypes"])
+def test_conversions_that_are_refused(way, monkeypatch):
+    if way == "ctypes":
+        monkeypatch.setattr(binding, "torch_call", lambda: None)
     with pytest.raises(ValueError):
         binding.quantize_mx4(torch.zeros(4, 4, dtype=torch.float16, device="cuda"))
     with pytest.raises(ValueError):

@@ -342,7 +342,42 @@ def test_a_step_of_training_the_routing_and_then_serving_in_4_bits():
 
 # ---- refusals
 
-def test_calls_that_are_refused():
+@pytest.fixture(params=["module", "ctypes"])
+def call(request, monkeypatch):
+    """The calls through the CPython module, and as they are made where that has not been built."""
+    if request.param == "ctypes":
+        monkeypatch.setattr(binding, "torch_call", lambda: None)
+    else:
+        assert binding.torch_call() is not None
+
+
+def test_both_ways_of_calling_give_the_same(call):
+    """Against the first way's results, on another stream too."""
+    depth, B = 5, 301
+    layer = tree(depth)
+    mix, leaf, mask = gpu(mixture(B, depth, 2, 1.0)), gpu(leaves(B, depth, 2)), torch.arange(B, device="cuda") % 5 != 0
+    up, one = torch.randn(B, 32, device="cuda", generator=torch.Generator("cuda").manual_seed(1)), torch.ones((), device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    runs = []
+    for stream in (None, side):
+        loss, counts, mean = layer.balance_loss(mix.requires_grad_(), leaf, token_mask=mask, stream=stream)
+        side.synchronize()
+        d = layer.balance_loss_backward(leaf, counts, one, token_mask=mask.byte(), stream=stream)
+        z = layer.routing_backward(mix, dmixture=up, leaf_idx=leaf, counts=counts, dloss=one, token_mask=mask, stream=stream)
+        q = binding.quantize_mx4(up, want_values=True, stream=stream)
+        torch.cuda.synchronize()
+        assert not (loss.requires_grad or d.requires_grad or z.requires_grad)
+        runs.append((loss, counts, mean, d, z) + q)
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+    key = [t.detach().cpu() for t in runs[0]]
+    global _first_way
+    _first_way = globals().get("_first_way", key)
+    assert all(torch.equal(a, b) for a, b in zip(_first_way, key))
+    layer.close()
+
+
+def test_calls_that_are_refused(call):
     layer = tree(3)
     mix, leaf = torch.rand(10, 8, device="cuda"), torch.zeros(10, dtype=torch.int32, device="cuda")
     counts, one = torch.ones(8, dtype=torch.int32, device="cuda"), torch.ones(1, device="cuda")
