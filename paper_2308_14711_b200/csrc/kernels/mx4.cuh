@@ -39,6 +39,7 @@ template <typename T> __device__ __forceinline__ float load_float(const T* p) { 
 // How rows lie: whole blocks, i.e. one long run of 16-byte vectors; whole groups of eight columns, so that vectors start everywhere but
 // blocks may be cut; anything.
 enum : int { kMxWhole = 0, kMxGroups = 1, kMxAny = 2 };
+constexpr int kMxAtOnce = 2;
 
 // unit / d and its remainder; 32-bit where the numbers are (a 64-bit division is a call of 100 instructions).
 __device__ __forceinline__ int64_t mx_divide(int64_t unit, uint32_t d, bool small, uint32_t& rest) {
@@ -83,11 +84,12 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
     const int64_t nb = mx_scales(cols), cb = mx_code_bytes(cols), total = rows * nb * 4;
     const int64_t step = (int64_t)gridDim.x * blockDim.x;
     const bool small = total + 4 * step < ((int64_t)1 << 31);
-    constexpr int U = 2;                                   // groups whose loads are in flight
+    constexpr int U = kMxAtOnce;                           // groups whose loads are in flight
     // (whole warps: the shuffles below want all lanes; step is a multiple of 32, and so is the rounded total)
     const int64_t end = (total + 31) & ~(int64_t)31;
     for (int64_t u0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u0 < end; u0 += U * step) {
         float v[U][8];
+        uint4 raw[U][sizeof(T) / 2];
         int64_t at[U], row[U];
         uint32_t g[U];                                     // group of the row
         int n[U];                                          // elements of the group that exist
@@ -99,22 +101,28 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
             if (kRows != kMxWhole) row[u] = mx_divide(unit, (uint32_t)(nb * 4), small, g[u]);
             n[u] = unit >= total ? 0 : kRows == kMxWhole ? 8 : (int)max((int64_t)0, min((int64_t)8, cols - (int64_t)g[u] * 8));
             at[u] = kRows == kMxWhole ? unit * 8 : row[u] * cols + (int64_t)g[u] * 8;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[u][e] = 0.0f;
-            if (kRows != kMxAny) {
-                if (n[u]) {
-                    if constexpr (sizeof(T) == 2) {
-                        Elem<T>::load_vec(src + at[u], v[u]);
-                    } else {
-                        const float4 a = __ldcs(reinterpret_cast<const float4*>(src + at[u])), b = __ldcs(reinterpret_cast<const float4*>(src + at[u]) + 1);
-                        v[u][0] = a.x; v[u][1] = a.y; v[u][2] = a.z; v[u][3] = a.w; v[u][4] = b.x; v[u][5] = b.y; v[u][6] = b.z; v[u][7] = b.w;
-                    }
-                }
+            if constexpr (kRows != kMxAny) {
+                // (without a branch, which would have the next load wait: a group that does not exist reads the first one)
+                const uint4* from = reinterpret_cast<const uint4*>(src + (n[u] ? at[u] : 0));
+                raw[u][0] = __ldcs(from);
+                if constexpr (sizeof(T) == 4) raw[u][1] = __ldcs(from + 1);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < n[u]) v[u][e] = load_float(src + at[u] + e);
+                for (int e = 0; e < 8; ++e) v[u][e] = load_float(src + (e < n[u] ? at[u] + e : 0));
             }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if constexpr (kRows == kMxAny) {
+            } else if constexpr (sizeof(T) == 2) {
+                Elem<T>::unpack(raw[u][0], v[u]);
+            } else {
+                const uint32_t w[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w, raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e] = __uint_as_float(w[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u][e] = e < n[u] ? v[u][e] : 0.0f;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {

@@ -38,11 +38,13 @@ struct BalanceScratch {
     int* done;              // [tiles][groups + 1] + [1], zero between calls
 };
 
-// Leaf of a token, -1 if it does not count.  (Both loads are sent for at once.)
-__device__ __forceinline__ int counted_leaf(const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask, int64_t b, int n_leaves) {
-    const int leaf = leaf_idx ? __ldg(leaf_idx + b) : 0;
-    const int kept = mask ? __ldg(mask + b) : 1;
-    return (unsigned)leaf < (unsigned)n_leaves && kept ? leaf : -1;
+// What says whether a token counts.  (Loads without branches: a branch around one has the next one wait for it.)
+struct TokenFlags {
+    int leaf, kept;
+    __device__ __forceinline__ bool counts(int n_leaves) const { return (unsigned)leaf < (unsigned)n_leaves && kept; }
+};
+__device__ __forceinline__ TokenFlags token_flags(const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask, int64_t b) {
+    return TokenFlags{leaf_idx ? __ldg(leaf_idx + b) : 0, mask ? __ldg(mask + b) : 1};
 }
 
 // Grid (slices, tiles).  Every CTA adds up its rows of its columns and counts its rows' leaves among them; the last CTA of a tile
@@ -78,14 +80,11 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
     const float* base = mix + col0 + c * V;
     for (int64_t b = b0 + r; b < b1; b += (int64_t)U * down) {
         float m[U][V];
-        int leaf[U];
+        TokenFlags flags[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t row = b + (int64_t)u * down;
-            leaf[u] = row < b1 ? counted_leaf(leaf_idx, mask, row, n_leaves) : -1;
-#pragma unroll
-            for (int v = 0; v < V; ++v) m[u][v] = 0.0f;
-            if (row >= b1) continue;
+            const int64_t row = min(b + (int64_t)u * down, b1 - 1);      // (past the end: the last row again)
+            flags[u] = token_flags(leaf_idx, mask, row);
             if constexpr (V == 4) {
                 const float4 q = __ldcs(reinterpret_cast<const float4*>(base + row * n_leaves));
                 m[u][0] = q.x; m[u][1] = q.y; m[u][2] = q.z; m[u][3] = q.w;
@@ -95,12 +94,13 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            const bool in = b + (int64_t)u * down < b1 && flags[u].counts(n_leaves);
             // (rows that do not count are left out, not multiplied by zero: they may hold anything)
 #pragma unroll
-            for (int v = 0; v < V; ++v) acc[v] += leaf[u] >= 0 ? m[u][v] : 0.0f;
-            if (c == 0 && leaf[u] >= 0) {
+            for (int v = 0; v < V; ++v) acc[v] += in ? m[u][v] : 0.0f;
+            if (c == 0 && in) {
                 ++mine;
-                if ((unsigned)(leaf[u] - col0) < (unsigned)cols) atomicAdd(&s_hist[leaf[u] - col0], 1);
+                if ((unsigned)(flags[u].leaf - col0) < (unsigned)cols) atomicAdd(&s_hist[flags[u].leaf - col0], 1);
             }
         }
     }
@@ -277,21 +277,19 @@ k_balance_loss_backward(const int32_t* __restrict__ leaf_idx, const uint8_t* __r
     const int64_t per = (B + gridDim.x - 1) / gridDim.x, b0 = blockIdx.x * per, b1 = min(B, b0 + per);
     float* base = dmix + col0 + c * V;
     for (int64_t b = b0 + r; b < b1; b += (int64_t)U * down) {
-        bool in[U];
+        TokenFlags flags[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t row = b + (int64_t)u * down;
-            in[u] = row < b1 && counted_leaf(leaf_idx, mask, row, n_leaves) >= 0;
-        }
+        for (int u = 0; u < U; ++u) flags[u] = token_flags(leaf_idx, mask, min(b + (int64_t)u * down, b1 - 1));
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t row = b + (int64_t)u * down;
             if (row >= b1) break;
+            const bool in = flags[u].counts(n_leaves);
             if constexpr (V == 4)
                 __stcs(reinterpret_cast<float4*>(base + row * n_leaves),
-                       in[u] ? make_float4(slope[0], slope[1], slope[2], slope[3]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f));
+                       in ? make_float4(slope[0], slope[1], slope[2], slope[3]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f));
             else
-                __stcs(base + row * n_leaves, in[u] ? slope[0] : 0.0f);
+                __stcs(base + row * n_leaves, in ? slope[0] : 0.0f);
         }
     }
 }

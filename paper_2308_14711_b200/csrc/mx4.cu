@@ -30,7 +30,7 @@ unsigned spread(int64_t units, int threads, int sm_count, int per_sm) {
 
 template <typename T>
 cudaError_t quantize(const LaunchOn& on, const T* src, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales, T* values) {
-    const unsigned grid = spread((rows * mx_scales(cols) * 4 + 1) / 2, 256, on.sm_count, 8);
+    const unsigned grid = spread((rows * mx_scales(cols) * 4 + kMxAtOnce - 1) / kMxAtOnce, 256, on.sm_count, 8);
     const auto kern = cols % kMxBlock == 0 ? k_quantize_mx4<T, kMxWhole> : cols % 8 == 0 ? k_quantize_mx4<T, kMxGroups> : k_quantize_mx4<T, kMxAny>;
     return launch_on(on, kern, grid, 1, 256, 0, src, codes, scales, values, rows, cols);
 }

@@ -46,8 +46,7 @@ size_t balance_scratch_bytes(int64_t n_leaves) {
 
 cudaError_t balance_loss(const LaunchOn& on, const float* mixture, const int32_t* leaf_idx, const uint8_t* mask, float* loss,
                          int32_t* counts, float* mean, int64_t B, int64_t n_leaves, void* scratch) {
-    int S = slices_for(B, n_leaves, kBalThreads, 16, balance_max_slices(balance_tiles(n_leaves)));
-    if (S > kBalGroup && S <= 3 * kBalGroup) S = kBalGroup;      // (a second round of sums costs more than longer slices)
+    const int S = slices_for(B, n_leaves, kBalThreads, 8, balance_max_slices(balance_tiles(n_leaves)));
     const unsigned T = (unsigned)balance_tiles(n_leaves);
     return launch_on(on, n_leaves >= 4 ? k_balance_loss<4> : k_balance_loss<1>, (unsigned)S, T, kBalThreads, 0, mixture, leaf_idx, mask, loss,
                      counts, mean, B, (int)n_leaves, layout(scratch, n_leaves));
