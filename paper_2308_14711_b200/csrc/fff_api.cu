@@ -1525,8 +1525,20 @@ fff_status_t run_block_forward(fff_handle_s* h, const void* x, void* y, int32_t*
 // 1500, 43.2 against 30.9 at 2048; 2048 leaves of 12: 24.9 against 34.6, 35.1 against 35.8, 45.0 against 37.6.
 constexpr int64_t kTokenBlockMaxB = 512, kTokenBlockMaxBDeep = 2048, kTokenBlockMaxBytes = (int64_t)96 << 20;
 
+// The same for 4-bit leaf weights (three CTAs per SM).  us, a CTA per token and the launches of larger batches: 768 -> 768, 256 leaves of 12: 197
+// tokens 12.3 and 20.5, 500 20.5 and 21.2, 700 20.8 and 21.5, 1000 26.7 and 22.5; 1024 -> 1024, 2048 leaves of 32: 500 26.7 and 52.1, 1500
+// 49.2 and 61.5, 2000 61.5 and 70.5, 3000 86.0 and 77.8; 4096 leaves of 8: 2000 55.3 and 68.5, 3000 77.9 and 76.8; 512 -> 512, one leaf of
+// 32: 500 12.3 and 20.5, 1000 16.4 and 20.5, 1500 22.5 and 21.4.  A token expands all weights of its leaf for itself: wider leaves than
+// those count by their weights.
+bool use_mx4_tokens(const fff_handle_s* h, int64_t B) {
+    // (thin leaves: 1456 columns, 2048 leaves of one, 1964 tokens 57.3 and 46.1 with a warp per token)
+    const int64_t most = (h->ustages.size() >= 2 ? (h->mx.mma ? 14 : 6) : h->depth == 0 ? 8 : 4) * (int64_t)h->sm_count;
+    return fff::mx4_token_fits(h->mx) && B <= most && B * h->l * (h->D + h->O) <= (int64_t)1 << 27;
+}
+
 bool use_token_block(const fff_handle_s* h, int64_t B) {
-    if (h->w8 || h->mx4 || h->path != FFF_PATH_AUTO || !h->tune[FFF_TUNE_TOKEN_BLOCKS]) return false;
+    if (h->w8 || h->path != FFF_PATH_AUTO || !h->tune[FFF_TUNE_TOKEN_BLOCKS]) return false;
+    if (h->mx4) return use_mx4_tokens(h, B);
     if (fff::TokenBlockLayout{h->D, h->l, (int)h->esize}.total() > 100 * 1024) return false;
     const bool two_stages = use_tensor_leaf(h) && h->ustages.size() >= 2;
     if (two_stages) {
@@ -1542,6 +1554,12 @@ bool use_token_block(const fff_handle_s* h, int64_t B) {
 
 template <typename T>
 fff_status_t run_token_block(fff_handle_s* h, const void* x, void* y, int32_t* leaf_out, int32_t* leaf_out2, int64_t B, cudaStream_t st) {
+    if (h->mx4) {
+        if (fff::mx4_tokens(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->act, h->d_status}, h->node_w, h->node_b, h->depth, leaf_out,
+                            leaf_out2, B) != cudaSuccess)
+            return cudaGetLastError(), FFF_ERR_CUDA;
+        return launched(h, st, "forward_token_blocks_mx4");
+    }
     const size_t smem = fff::TokenBlockLayout{h->D, h->l, (int)h->esize}.total();
     static bool limit_raised[kMaxDevices] = {};
     if (smem > 48 * 1024 && !raise_smem_limit(fff::k_token_block<T>, h->device, 100 * 1024, limit_raised)) return FFF_ERR_CUDA;

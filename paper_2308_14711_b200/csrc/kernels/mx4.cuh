@@ -14,6 +14,7 @@
 
 #include "common.cuh"
 #include "ptx.cuh"
+#include "token_block.cuh"
 
 namespace fff {
 
@@ -407,9 +408,9 @@ __device__ __forceinline__ void mx_fetch_codes(const unsigned char* __restrict__
         q.sc[k][h] = __ldg(rec + at_s1 + row * 2 + (c >> 1));
     }
 }
-template <bool kBig>
+template <bool kBig, int G>
 __device__ __forceinline__ void mx_hidden(const unsigned char* __restrict__ rec, int at_s1, int l, MxCodes& q, const unsigned char* xs, int pitch,
-                                          int groups, int row0, int u0, int u1, int step, int unit_base, int lane, float (&acc)[kMxMaxGroups][4])
+                                          int groups, int row0, int u0, int u1, int step, int unit_base, int lane, float (&acc)[G][4])
 {
     const int g = lane >> 2, c = lane & 3;
     for (int u = u0; u < u1; u += kMxAhead * step) {
@@ -424,7 +425,7 @@ __device__ __forceinline__ void mx_hidden(const unsigned char* __restrict__ rec,
             const unsigned char* xp = xs + g * pitch + (uk - unit_base) * (kMxUnit * 2) + 32 * c;
             // (two groups at a time, whose MMAs do not wait for one another; a last odd group is computed twice)
 #pragma unroll
-            for (int t = 0; t < kMxMaxGroups; t += 2) {
+            for (int t = 0; t < G; t += 2) {
                 if (t >= groups) break;
                 const unsigned char *xa = xp + t * 8 * pitch, *xb = t + 1 < groups ? xa + 8 * pitch : xa;
                 const uint4 a0 = *reinterpret_cast<const uint4*>(xa), b0 = *reinterpret_cast<const uint4*>(xb);
@@ -437,6 +438,142 @@ __device__ __forceinline__ void mx_hidden(const unsigned char* __restrict__ rec,
                 ptx::mma_bf16(acc[t + 1], w[0][4], w[1][4], w[0][5], w[1][5], b1.x, b1.y);
                 ptx::mma_bf16(acc[t], w[0][6], w[1][6], w[0][7], w[1][7], a1.z, a1.w);
                 ptx::mma_bf16(acc[t + 1], w[0][6], w[1][6], w[0][7], w[1][7], b1.z, b1.w);
+            }
+        }
+    }
+}
+
+// The raw operands of a K-block of 64 outputs, and the outputs' biases.
+struct MxNext {
+    uint4 q0, q1, bias;
+    uint2 sc;
+};
+template <bool K16>
+__device__ __forceinline__ void mx_fetch_outputs(const MxLayout& Ly, const unsigned char* __restrict__ rec, int u, int kb, int lane, MxNext& next) {
+    if (u >= Ly.units2()) return;
+    const int g = lane >> 2, c = lane & 3, Kp = K16 ? 16 : Ly.Kp();
+    const uint4* src = reinterpret_cast<const uint4*>(rec + Ly.at_w2()) + (K16 ? u * 32 : (u * (Kp / 32) + kb) * 64) + lane;
+    const unsigned char* sp = rec + Ly.at_s2() + (u * 2 + (g >> 2)) * Kp + kb * 32 + (K16 ? 4 : 8) * c;
+    next.q0 = __ldg(src);
+    if constexpr (K16) {
+        next.sc.x = __ldg(reinterpret_cast<const uint32_t*>(sp));
+    } else {
+        next.q1 = __ldg(src + 32);
+        next.sc = __ldg(reinterpret_cast<const uint2*>(sp));
+    }
+    if (kb == 0 && u * kMxUnit + 8 * g < Ly.O)             // (to the end of 16 bytes: records are padded)
+        next.bias = __ldg(reinterpret_cast<const uint4*>(rec + Ly.at_b2()) + u * 8 + g);
+}
+
+// The second product: units u0, u0 + step, .. of 64 outputs for all tokens of a tile, by one warp; numbered so that a lane ends with 8
+// consecutive outputs of its tokens and 8 lanes with 128 bytes of a row.  hid: hidden values [2][R][Kp] (the two summands of each);
+// next: the operands of (u0, 0), fetched before.  TG token groups at a time: their MMAs do not wait for one another (a last odd group is
+// computed twice), and wider leaves expand every K-block once for all of them.
+template <bool K16, bool kWide, bool kBig, int TG>
+__device__ __forceinline__ void mx_outputs(__nv_bfloat16* __restrict__ y, bool y_vec, const MxLayout& Ly, const unsigned char* __restrict__ rec,
+                                           const __nv_bfloat16* hid, int R, int rows, const int* s_tok, int u0, int step, int lane, MxNext& next)
+{
+    constexpr int P = K16 ? 2 : 4;
+    const int g = lane >> 2, c = lane & 3, O = Ly.O, units2 = Ly.units2(), Kp = K16 ? 16 : kWide ? Ly.Kp() : 32, kblocks = kWide ? Kp / 32 : 1;
+    const int groups = (rows + 7) / 8;
+    auto fetch = [&](int u, int kb) { mx_fetch_outputs<K16>(Ly, rec, u, kb, lane, next); };
+    for (int u = u0; u < units2; u += step) {
+        const int o = u * kMxUnit + 8 * g, n = O - o;
+        // biases as the sums that the MMAs start from: outputs 2 i and 2 i + 1 of two tokens
+        float bias[4][4];
+        {
+            const uint32_t bw[4] = {next.bias.x, next.bias.y, next.bias.z, next.bias.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                bias[i][0] = bias[i][1] = __uint_as_float(bw[i] << 16);
+                bias[i][2] = bias[i][3] = __uint_as_float(bw[i] & 0xffff0000u);
+            }
+        }
+        uint32_t w[8][P];                              // [2 i + row][pair of hidden units]
+        auto operands = [&]() {
+            uint32_t f1[P], f2[P];                     // the scales of a pair of hidden units are neighbouring bytes
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const uint32_t two = p < 2 ? next.sc.x : next.sc.y, lo = (two >> (16 * (p & 1))) & 0xffu, hi = (two >> (16 * (p & 1) + 8)) & 0xffu;
+                f1[p] = mx_pair(mx_mul1(lo, kBig), mx_mul1(hi, kBig));
+                f2[p] = kBig ? mx_pair(mx_mul2(lo), mx_mul2(hi)) : 0u;
+            }
+            const uint32_t q[8] = {next.q0.x, next.q0.y, next.q0.z, next.q0.w, next.q1.x, next.q1.y, next.q1.z, next.q1.w};
+#pragma unroll
+            for (int i = 0; i < (K16 ? 4 : 8); ++i) {
+                uint32_t r[4];
+                mx_expand(q[i], r);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int row = K16 ? 2 * i + (k >> 1) : i, p = K16 ? k & 1 : k;
+                    w[row][p] = mul_bf16x2(r[k], f1[p]);
+                    if (kBig) w[row][p] = mul_bf16x2(w[row][p], f2[p]);
+                }
+            }
+        };
+        if (!kWide) {
+            operands();
+            fetch(u + step, 0);
+        }
+        for (int t0 = 0; t0 < groups; t0 += TG) {
+            float acc[TG][4][4];
+            const __nv_bfloat16* h[TG];
+#pragma unroll
+            for (int t = 0; t < TG; ++t) {
+                h[t] = hid + (8 * (t0 + t < groups ? t0 + t : t0) + g) * Kp + (K16 ? 4 : 8) * c;
+                if constexpr (kWide) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[t][i][k] = bias[i][k];
+                }
+            }
+            // outputs 2 i and 2 i + 1 of every token group, from pair `pair` of the hidden units on; the first to come takes the biases
+            auto multiply = [&](int pair, const uint32_t (&b)[TG][2], bool first) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int t = 0; t < TG; ++t) {
+                        if (first) ptx::mma_bf16_from(acc[t][i], bias[i], w[2 * i][pair], w[2 * i + 1][pair], w[2 * i][pair + 1], w[2 * i + 1][pair + 1], b[t][0], b[t][1]);
+                        else ptx::mma_bf16(acc[t][i], w[2 * i][pair], w[2 * i + 1][pair], w[2 * i][pair + 1], w[2 * i + 1][pair + 1], b[t][0], b[t][1]);
+                    }
+            };
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (kWide) {
+                    operands();
+                    if (kb + 1 < kblocks) fetch(u, kb + 1);
+                    else fetch(t0 + TG < groups ? u : u + step, 0);
+                }
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    uint32_t b[2][TG][2];
+#pragma unroll
+                    for (int t = 0; t < TG; ++t) {
+                        const __nv_bfloat16* from = h[t] + p * R * Kp + kb * 32;
+                        if constexpr (K16) {
+                            const uint2 q = *reinterpret_cast<const uint2*>(from);
+                            b[0][t][0] = q.x; b[0][t][1] = q.y;
+                        } else {
+                            const uint4 q = *reinterpret_cast<const uint4*>(from);
+                            b[0][t][0] = q.x; b[0][t][1] = q.y; b[1][t][0] = q.z; b[1][t][1] = q.w;
+                        }
+                    }
+                    multiply(0, b[0], !kWide && p == 0);
+                    if constexpr (!K16) multiply(2, b[1], false);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < TG; ++t) {
+                if (t0 + t >= groups) break;
+                const int2 tok = *reinterpret_cast<const int2*>(s_tok + 8 * (t0 + t) + 2 * c);
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const int to = r ? tok.y : tok.x;
+                    uint32_t out[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) out[i] = ptx::pack_bf16(acc[t][i][r], acc[t][i][2 + r]);
+                    if (8 * (t0 + t) + 2 * c + r < rows) mx_store8(y + (int64_t)to * O + o, n, y_vec, out);
+                }
             }
         }
     }
@@ -459,8 +596,7 @@ __device__ __forceinline__ int mx_bin_of_tile(const uint16_t* pre, int n_bins, i
 // sent for as soon as this tile's first product is done with the buffer, and arrive while its hidden values and outputs are computed;
 // the next leaf's record is sent for to L2 at the same time.  The first product is split along D over the warps (MT = 2: over the two
 // groups of 16 hidden units too), so that no weight is expanded twice; the sums meet in shared memory, where bias and activation are
-// applied; for the second product every warp has output columns of its own, numbered so that a lane ends with 8 consecutive outputs
-// of its tokens and 8 lanes with 128 bytes of a row.  Hidden values are kept as sums of two bf16 values (float32 precision to 2^-16):
+// applied; for the second product every warp has output columns of its own.  Hidden values are kept as sums of two bf16 values (float32 precision to 2^-16):
 // the extra MMAs cost little next to the expansion.
 // MT: groups of 16 hidden units at a time: 1 for leaves of up to 16 (one K-block of 16 in the second product), else 2.
 // kWide: more than 32 hidden units: several passes over x, several K-blocks in the second product.
@@ -470,13 +606,13 @@ k_leaf_mx4(const MxLeafArgs A)
 {
     static_assert(!kWide || MT == 2, "leaves of up to 16 have one K-block");
     constexpr bool K16 = MT == 1;
-    constexpr int NW = kMxWarps, kThreads = kMxThreads, P = K16 ? 2 : 4;
+    constexpr int NW = kMxWarps, kThreads = kMxThreads;
     constexpr int kSplit = NW / MT;                        // warps that share a group of 16 hidden units
     extern __shared__ __align__(16) unsigned char smem_mx[];
     __shared__ int s_wsum[NW], s_last, s_next[2][3];       // s_next: tile, leaf, rows
     __shared__ uint64_t s_full;
     const MxLayout& Ly = A.lay;
-    const int l = Ly.l, D = Ly.D, O = Ly.O, Kp = K16 ? 16 : kWide ? Ly.Kp() : 32;
+    const int l = Ly.l, D = Ly.D, Kp = K16 ? 16 : kWide ? Ly.Kp() : 32;
     const int R = A.tile_rows;
     const MxLeafSmem S{R, D, Kp, A.counts ? A.n_leaves : 0};
     unsigned char* xs = smem_mx;
@@ -504,9 +640,8 @@ k_leaf_mx4(const MxLeafArgs A)
             return n;
         }, A.n_leaves, R, s_pre, s_wsum, kThreads);
     const int n_tiles = A.counts ? s_pre[A.n_leaves] : A.n_tiles;
-    const int units1 = Ly.units1(), units2 = Ly.units2(), kblocks = kWide ? Kp / 32 : 1;
+    const int units1 = Ly.units1(), at_s1 = Ly.at_s1(), at_b1 = Ly.at_b1();
     const int64_t record = Ly.record();
-    const int at_s1 = Ly.at_s1(), at_w2 = Ly.at_w2(), at_s2 = Ly.at_s2(), at_b1 = Ly.at_b1(), at_b2 = Ly.at_b2();
     const bool bulk = A.x_bytes >= 16;
 
     // The first tile from `tile` on that is not empty (a list of tiles may contain empty ones); rows = 0: none.  Tokens `lane` and
@@ -588,22 +723,7 @@ k_leaf_mx4(const MxLeafArgs A)
         const unsigned char* rec = A.image + leaf * record;
         if (warp == kFinder) following = find_tile(tile + gridDim.x);
 
-        // the raw operands of a K-block of 64 outputs, and the outputs' biases
-        struct { uint4 q0, q1, bias; uint2 sc; } next;
-        auto fetch = [&](int u, int kb) {
-            if (u >= units2) return;
-            const uint4* src = reinterpret_cast<const uint4*>(rec + at_w2) + (u * kblocks + kb) * (K16 ? 32 : 64) + lane;
-            const unsigned char* sp = rec + at_s2 + (u * 2 + (g >> 2)) * Kp + kb * 32 + (K16 ? 4 : 8) * c;
-            next.q0 = __ldg(src);
-            if constexpr (K16) {
-                next.sc.x = __ldg(reinterpret_cast<const uint32_t*>(sp));
-            } else {
-                next.q1 = __ldg(src + 32);
-                next.sc = __ldg(reinterpret_cast<const uint2*>(sp));
-            }
-            if (kb == 0 && u * kMxUnit + 8 * g < O)        // (to the end of 16 bytes: records are padded)
-                next.bias = __ldg(reinterpret_cast<const uint4*>(rec + at_b2) + u * 8 + g);
-        };
+        MxNext next;
 
         // ---- hidden values
         for (int unit0 = 0; unit0 < l; unit0 += 16 * MT) {
@@ -640,7 +760,7 @@ k_leaf_mx4(const MxLeafArgs A)
                     }
                     __syncthreads();
                 }
-                mx_hidden<kBig>(rec, at_s1, l, q, xs, pitch, groups, row0, u0, u1, kSplit, ub, lane, acc);
+                mx_hidden<kBig, kMxMaxGroups>(rec, at_s1, l, q, xs, pitch, groups, row0, u0, u1, kSplit, ub, lane, acc);
             }
 #pragma unroll
             for (int t = 0; t < kMxMaxGroups; ++t) {
@@ -651,7 +771,7 @@ k_leaf_mx4(const MxLeafArgs A)
             __syncthreads();
             if (last_pass) {
                 if (warp == kFinder) announce(following, buf ^ 1);
-                fetch(warp, 0);
+                mx_fetch_outputs<K16>(Ly, rec, warp, 0, lane, next);
             }
             with_activation(A.act, [&](auto act) {
                 const float* from = red + (my_m * kSplit * groups * 4 + my_i) * 32 + lane;
@@ -673,115 +793,7 @@ k_leaf_mx4(const MxLeafArgs A)
         }
 
         // ---- outputs
-        for (int u = warp; u < units2; u += NW) {
-            const int o = u * kMxUnit + 8 * g, n = O - o;
-            // biases as the sums that the MMAs start from: outputs 2 i and 2 i + 1 of two tokens
-            float bias[4][4];
-            {
-                const uint32_t bw[4] = {next.bias.x, next.bias.y, next.bias.z, next.bias.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    bias[i][0] = bias[i][1] = __uint_as_float(bw[i] << 16);
-                    bias[i][2] = bias[i][3] = __uint_as_float(bw[i] & 0xffff0000u);
-                }
-            }
-            uint32_t w[8][P];                              // [2 i + row][pair of hidden units]
-            auto operands = [&]() {
-                uint32_t f1[P], f2[P];                     // the scales of a pair of hidden units are neighbouring bytes
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    const uint32_t two = p < 2 ? next.sc.x : next.sc.y, lo = (two >> (16 * (p & 1))) & 0xffu, hi = (two >> (16 * (p & 1) + 8)) & 0xffu;
-                    f1[p] = mx_pair(mx_mul1(lo, kBig), mx_mul1(hi, kBig));
-                    f2[p] = kBig ? mx_pair(mx_mul2(lo), mx_mul2(hi)) : 0u;
-                }
-                const uint32_t q[8] = {next.q0.x, next.q0.y, next.q0.z, next.q0.w, next.q1.x, next.q1.y, next.q1.z, next.q1.w};
-#pragma unroll
-                for (int i = 0; i < (K16 ? 4 : 8); ++i) {
-                    uint32_t r[4];
-                    mx_expand(q[i], r);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int row = K16 ? 2 * i + (k >> 1) : i, p = K16 ? k & 1 : k;
-                        w[row][p] = mul_bf16x2(r[k], f1[p]);
-                        if (kBig) w[row][p] = mul_bf16x2(w[row][p], f2[p]);
-                    }
-                }
-            };
-            if (!kWide) {
-                operands();
-                fetch(u + NW, 0);
-            }
-            // two token groups at a time, whose MMAs do not wait for one another (a last odd group is computed twice); wider leaves expand
-            // every K-block once for both
-            constexpr int TG = 2;
-            for (int t0 = 0; t0 < groups; t0 += TG) {
-                float acc[TG][4][4];
-                if constexpr (kWide) {
-#pragma unroll
-                    for (int t = 0; t < TG; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) acc[t][i][k] = bias[i][k];
-                }
-                const __nv_bfloat16* ha = hid + (8 * t0 + g) * Kp + (K16 ? 4 : 8) * c;
-                const __nv_bfloat16* hb = t0 + 1 < groups ? ha + 8 * Kp : ha;
-                for (int kb = 0; kb < kblocks; ++kb) {
-                    if (kWide) {
-                        operands();
-                        if (kb + 1 < kblocks) fetch(u, kb + 1);
-                        else fetch(t0 + TG < groups ? u : u + NW, 0);
-                    }
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        if constexpr (K16) {
-                            const uint2 b0 = *reinterpret_cast<const uint2*>(ha + p * R * Kp), b1 = *reinterpret_cast<const uint2*>(hb + p * R * Kp);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if (p == 0) {
-                                    ptx::mma_bf16_from(acc[0][i], bias[i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b0.x, b0.y);
-                                    ptx::mma_bf16_from(acc[1][i], bias[i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b1.x, b1.y);
-                                } else {
-                                    ptx::mma_bf16(acc[0][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b0.x, b0.y);
-                                    ptx::mma_bf16(acc[1][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b1.x, b1.y);
-                                }
-                            }
-                        } else {
-                            const uint4 b0 = *reinterpret_cast<const uint4*>(ha + p * R * Kp + kb * 32);
-                            const uint4 b1 = *reinterpret_cast<const uint4*>(hb + p * R * Kp + kb * 32);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if (!kWide && p == 0) {
-                                    ptx::mma_bf16_from(acc[0][i], bias[i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b0.x, b0.y);
-                                    ptx::mma_bf16_from(acc[1][i], bias[i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b1.x, b1.y);
-                                } else {
-                                    ptx::mma_bf16(acc[0][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b0.x, b0.y);
-                                    ptx::mma_bf16(acc[1][i], w[2 * i][0], w[2 * i + 1][0], w[2 * i][1], w[2 * i + 1][1], b1.x, b1.y);
-                                }
-                            }
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                ptx::mma_bf16(acc[0][i], w[2 * i][2], w[2 * i + 1][2], w[2 * i][3], w[2 * i + 1][3], b0.z, b0.w);
-                                ptx::mma_bf16(acc[1][i], w[2 * i][2], w[2 * i + 1][2], w[2 * i][3], w[2 * i + 1][3], b1.z, b1.w);
-                            }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < TG; ++t) {
-                    if (t0 + t >= groups) break;
-                    const int2 tok = *reinterpret_cast<const int2*>(s_tok + 8 * (t0 + t) + 2 * c);
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const int to = r ? tok.y : tok.x;
-                        uint32_t out[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) out[i] = ptx::pack_bf16(acc[t][i][r], acc[t][i][2 + r]);
-                        if (to >= 0) mx_store8(A.y + (int64_t)to * O + o, n, A.y_bytes == 16, out);
-                    }
-                }
-            }
-        }
+        mx_outputs<K16, kWide, kBig, 2>(A.y, A.y_bytes == 16, Ly, rec, hid, R, rows, s_tok, warp, NW, lane, next);
         mine = following;
     }
     if (timed_out) {
@@ -799,6 +811,93 @@ k_leaf_mx4(const MxLeafArgs A)
         if (s_last)
             for (int b = tid; b <= A.n_leaves; b += kThreads) A.counts[b] = 0;
     }
+}
+
+// ---- a few tokens ----------------------------------------------------------------------------------
+
+struct MxTokenArgs {
+    const __nv_bfloat16 *x, *node_w, *node_b;
+    const unsigned char* image;
+    __nv_bfloat16* y;
+    int32_t *leaf_out, *leaf_out2;     // (leaf_out2 may be nullptr)
+    MxLayout lay;
+    int depth, act;
+    bool x_vec, y_vec, big;            // rows of x / y are 16-byte vectors; (k_mx4_token_rows) some scale is over 2
+};
+
+// Shared memory: the token's row padded with zeros, partial sums, hidden values (eight rows of them: the operand of an MMA).
+struct MxTokenSmem {
+    int D, Kp;
+    __host__ __device__ int x() const { return (D + kMxUnit - 1) / kMxUnit * kMxUnit * 2; }
+    __host__ __device__ int bytes() const { return x() + kTBWarps * 512 + 8 * Kp * 4; }
+};
+
+// As k_token_block: a CTA walks one token down the tree and evaluates its leaf, with the arithmetic of k_leaf_mx4 on one token (its row
+// is every column of the MMAs' operand; what the other seven columns give is not stored).  Three CTAs per SM (80 registers, a few
+// spilled): two are 2 us ahead up to two per SM and a fifth behind from then on, four behind everywhere.
+template <int MT, bool kWide, bool kBig>
+__global__ void __launch_bounds__(kTBThreads, 3)
+k_mx4_token(const MxTokenArgs A)
+{
+    using T = __nv_bfloat16;
+    constexpr bool K16 = MT == 1;
+    constexpr int NW = kTBWarps, kSplit = NW / MT;
+    extern __shared__ __align__(16) unsigned char smem_mt[];
+    __shared__ float s_logit[2][8];
+    __shared__ int s_tok[8];
+    const MxLayout& Ly = A.lay;
+    const int D = Ly.D, l = Ly.l, Kp = K16 ? 16 : kWide ? Ly.Kp() : 32;
+    const MxTokenSmem S{D, Kp};
+    T* xs = reinterpret_cast<T*>(smem_mt);
+    float* red = reinterpret_cast<float*>(smem_mt + S.x());              // [warp][register][lane]
+    T* hid = reinterpret_cast<T*>(smem_mt + S.x() + NW * 512);           // [2][8][Kp]
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
+    TokenWalk<T> walk;
+    walk.send_first(A.node_w, A.node_b, D, A.depth, A.x_vec, warp, lane);
+    for (int i = D + tid; i < S.x() / 2; i += kTBThreads) xs[i] = __float2bfloat16_rn(0.0f);
+    if (tid < 8) s_tok[tid] = blockIdx.x;
+    pdl_trigger();
+    pdl_wait();
+    const T* xt = A.x + (int64_t)blockIdx.x * D;
+    if (A.x_vec) {
+        for (int i = tid; i < D / 8; i += kTBThreads) reinterpret_cast<uint4*>(xs)[i] = __ldg(reinterpret_cast<const uint4*>(xt) + i);
+    } else {
+        for (int i = tid; i < D; i += kTBThreads) xs[i] = xt[i];
+    }
+    __syncthreads();
+    const int64_t leaf = walk.leaf(A.node_w, A.node_b, xs, D, A.depth, A.x_vec, warp, lane, s_logit);
+    if (tid == 0) {
+        A.leaf_out[blockIdx.x] = (int32_t)leaf;
+        if (A.leaf_out2) A.leaf_out2[blockIdx.x] = (int32_t)leaf;
+    }
+    const unsigned char* rec = A.image + leaf * Ly.record();
+    const int at_s1 = Ly.at_s1(), at_b1 = Ly.at_b1(), units1 = Ly.units1();
+    MxNext next;
+    for (int unit0 = 0; unit0 < l; unit0 += 16 * MT) {
+        const int row0 = unit0 + 16 * (warp / kSplit), u0 = warp % kSplit;
+        MxCodes q;
+#pragma unroll
+        for (int k = 0; k < kMxAhead; ++k) mx_fetch_codes(rec, at_s1, l, row0, u0 + k * kSplit, units1, lane, q, k);
+        if (unit0 == 0) mx_fetch_outputs<K16>(Ly, rec, warp, 0, lane, next);
+        float acc[2][4] = {};
+        mx_hidden<kBig, 2>(rec, at_s1, l, q, reinterpret_cast<const unsigned char*>(xs), 0, 1, row0, u0, units1, kSplit, 0, lane, acc);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red[(warp * 4 + i) * 32 + lane] = acc[0][i];
+        __syncthreads();
+        for (int f = warp; f < 4 * MT; f += NW) {          // unit group, register; the lane is the lane
+            const int m = f >> 2, i = f & 3, unit = unit0 + 16 * m + g + 8 * (i >> 1), row = 2 * c + (i & 1);
+            float sum = unit < l ? __bfloat162float(__ldg(reinterpret_cast<const T*>(rec + at_b1) + unit)) : 0.0f;
+#pragma unroll
+            for (int w = 0; w < kSplit; ++w) sum += red[((m * kSplit + w) * 4 + i) * 32 + lane];
+            const float h = unit < l ? activate_bf16(A.act, sum) : 0.0f;
+            const T hi = __float2bfloat16_rn(h);
+            const float f32 = __bfloat162float(hi);
+            hid[row * Kp + unit] = hi;
+            hid[(8 + row) * Kp + unit] = __float2bfloat16_rn(isinf(f32) ? 0.0f : h - f32);
+        }
+        __syncthreads();
+    }
+    mx_outputs<K16, kWide, kBig, 1>(A.y, A.y_vec, Ly, rec, hid, 8, 1, s_tok, warp, NW, lane, next);
 }
 
 // ---- thin leaves on CUDA cores ---------------------------------------------------------------------
@@ -922,6 +1021,73 @@ k_leaf_mx4_rows(const MxRowsArgs A)
             }
         }
         __syncwarp();
+    }
+}
+
+// The same for a few tokens, as k_mx4_token: a CTA per token, a warp per hidden unit, a thread per eight outputs.
+__global__ void __launch_bounds__(kTBThreads, 4)
+k_mx4_token_rows(const MxTokenArgs A)
+{
+    using T = __nv_bfloat16;
+    extern __shared__ __align__(16) unsigned char smem_mt[];
+    __shared__ float s_logit[2][8], s_h[8];
+    const MxLayout& Ly = A.lay;
+    const int D = Ly.D, O = Ly.O, l = Ly.l, wd = (D + 7) / 8, wo = (O + 7) / 8;
+    T* xs = reinterpret_cast<T*>(smem_mt);                 // [8 wd]
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    TokenWalk<T> walk;
+    walk.send_first(A.node_w, A.node_b, D, A.depth, A.x_vec, warp, lane);
+    if (tid < 8 * wd - D) xs[D + tid] = __float2bfloat16_rn(0.0f);
+    pdl_trigger();
+    pdl_wait();
+    const T* xt = A.x + (int64_t)blockIdx.x * D;
+    if (A.x_vec) {
+        for (int i = tid; i < D / 8; i += kTBThreads) reinterpret_cast<uint4*>(xs)[i] = __ldg(reinterpret_cast<const uint4*>(xt) + i);
+    } else {
+        for (int i = tid; i < D; i += kTBThreads) xs[i] = xt[i];
+    }
+    __syncthreads();
+    const int64_t leaf = walk.leaf(A.node_w, A.node_b, xs, D, A.depth, A.x_vec, warp, lane, s_logit);
+    if (tid == 0) {
+        A.leaf_out[blockIdx.x] = (int32_t)leaf;
+        if (A.leaf_out2) A.leaf_out2[blockIdx.x] = (int32_t)leaf;
+    }
+    const unsigned char* rec = A.image + leaf * Ly.record();
+    if (tid == 0) mx_prefetch(rec, Ly.record());
+    if (warp < l) {
+        const uint32_t* w1 = reinterpret_cast<const uint32_t*>(rec) + warp * wd;
+        const unsigned char* s1 = rec + Ly.at_s1() + warp * (int)mx_scales(D);
+        float sum = 0.0f;
+#pragma unroll 4
+        for (int w = lane; w < wd; w += 32) {
+            float v[8], xv[8];
+            mx_floats(__ldg(w1 + w), __ldg(s1 + (w >> 2)), A.big, v);
+            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + 8 * w), xv);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(v[e], xv[e], sum);
+        }
+        sum = warp_sum(sum);
+        if (lane == 0) s_h[warp] = activate(A.act, sum + __bfloat162float(reinterpret_cast<const T*>(rec + Ly.at_b1())[warp]));
+    }
+    __syncthreads();
+    const uint32_t* w2 = reinterpret_cast<const uint32_t*>(rec + Ly.at_w2());
+    const unsigned char* s2 = rec + Ly.at_s2();
+    const int no = (int)mx_scales(O);
+    T* yt = A.y + (int64_t)blockIdx.x * O;
+    for (int w = tid; w < wo; w += kTBThreads) {
+        float acc[8];
+        Elem<T>::load_vec(reinterpret_cast<const T*>(rec + Ly.at_b2()) + 8 * w, acc);
+#pragma unroll 4
+        for (int q = 0; q < l; ++q) {
+            float v[8];
+            mx_floats(__ldg(w2 + q * wo + w), __ldg(s2 + q * no + (w >> 2)), A.big, v);
+            const float hq = s_h[q];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = fmaf(v[e], hq, acc[e]);
+        }
+        const uint32_t out[4] = {ptx::pack_bf16(acc[0], acc[1]), ptx::pack_bf16(acc[2], acc[3]), ptx::pack_bf16(acc[4], acc[5]),
+                                 ptx::pack_bf16(acc[6], acc[7])};
+        mx_store8(yt + 8 * w, O - 8 * w, A.y_vec, out);
     }
 }
 

@@ -85,6 +85,71 @@ __device__ __forceinline__ void token_dots(const T* const (&rows)[N], const T* _
     for (int n = 0; n < N; ++n) out[n] = warp_sum(out[n]);
 }
 
+// The walk of one token, by a CTA of kTBWarps warps.
+// The first step's nodes are the same for every token, and parameters: their rows are sent for before the kernel waits for its
+// predecessor, and arrive while x does: one image of 768 columns 8.6 -> 7.9 us, 102 float32 tokens of 832 7.9 -> 7.35.  Rows of up to the
+// 1024 columns that stay in registers.
+template <typename T>
+struct TokenWalk {
+    static constexpr int U = kTBAhead<T>, V = Elem<T>::kVec;
+    uint4 top_row[U];
+    float top_bias;
+    bool ahead, has_top;
+    __device__ __forceinline__ void send_first(const T* __restrict__ node_w, const T* __restrict__ node_b, int D, int depth, bool vec, int warp, int lane) {
+        ahead = vec && D <= 32 * V * U;
+        has_top = ahead && warp < (1 << min(kTBLevels, depth)) - 1;
+        top_bias = 0.0f;
+        if (has_top) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = (u * 32 + lane) * V;
+                top_row[u] = k < D ? __ldg(reinterpret_cast<const uint4*>(node_w + (int64_t)warp * D + k)) : make_uint4(0u, 0u, 0u, 0u);
+            }
+            top_bias = Elem<T>::to_float(node_b[warp]);
+        }
+    }
+    // xs: the token's row in shared memory, s_logit: [2][8] floats there
+    __device__ __forceinline__ int64_t leaf(const T* __restrict__ node_w, const T* __restrict__ node_b, const T* xs, int D, int depth, bool vec,
+                                            int warp, int lane, float (&s_logit)[2][8]) {
+        int64_t n = 0;
+        if (has_top) {                                  // (summed as in token_dots)
+            float sum = 0.0f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = (u * 32 + lane) * V;
+                if (k >= D) break;
+                float xv[V], wv[V];
+                Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + k), xv);
+                Elem<T>::unpack(top_row[u], wv);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum = fmaf(wv[e], xv[e], sum);
+            }
+            sum = warp_sum(sum);
+            if (lane == 0) s_logit[0][warp] = sum + top_bias;
+        }
+        for (int m = 0, buf = 0; m < depth; m += kTBLevels, buf ^= 1) {
+            const int r = min(kTBLevels, depth - m);
+            if (warp < (1 << r) - 1 && !(m == 0 && ahead)) {
+                const int lev = 31 - __clz(warp + 1);
+                const int64_t row = (((int64_t)1 << (m + lev)) - 1) + (n << lev) + (warp + 1 - (1 << lev));
+                const T* rows[1] = {node_w + row * D};
+                const float bias = Elem<T>::to_float(node_b[row]);
+                float sum[1];
+                token_dots<T, 1>(rows, xs, D, vec, lane, sum);
+                if (lane == 0) s_logit[buf][warp] = sum[0] + bias;
+            }
+            __syncthreads();
+            int p = 0;
+            for (int i = 0; i < r; ++i) {
+                const int right = s_logit[buf][p] >= 0.0f ? 1 : 0;
+                p = 2 * p + 1 + right;
+                n = 2 * n + right;
+            }
+        }
+        return n;
+    }
+};
+
 // leaf_out / leaf_out2 (optional): leaf of every token.
 template <typename T>
 __global__ void __launch_bounds__(kTBThreads, sizeof(T) == 2 ? 4 : 2)
@@ -104,21 +169,8 @@ k_token_block(const T* __restrict__ x, const T* __restrict__ node_w, const T* __
     const int row_bytes = l * (int)sizeof(T);
     const int stage_rows = ((int64_t)O * row_bytes) % 16 == 0 ? (kTBW2Bytes / row_bytes) & ~15 : 0;
 
-    // The first step's nodes are the same for every token, and parameters: their rows are sent for before the kernel waits for its
-    // predecessor, and arrive while x does: one image of 768 columns 8.6 -> 7.9 us, 102 float32 tokens of 832 7.9 -> 7.35.  Rows of up to the
-    // 1024 columns that stay in registers.
-    constexpr int U = kTBAhead<T>;
-    const bool ahead = vec && D <= 32 * V * U, has_top = ahead && warp < (1 << min(kTBLevels, depth)) - 1;
-    uint4 top_row[U];
-    float top_bias = 0.0f;
-    if (has_top) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = (u * 32 + lane) * V;
-            top_row[u] = k < D ? __ldg(reinterpret_cast<const uint4*>(node_w + (int64_t)warp * D + k)) : make_uint4(0u, 0u, 0u, 0u);
-        }
-        top_bias = Elem<T>::to_float(node_b[warp]);
-    }
+    TokenWalk<T> walk;
+    walk.send_first(node_w, node_b, D, depth, vec, warp, lane);
     pdl_trigger();
     pdl_wait();
     const int t = blockIdx.x;                           // (a CTA per token)
@@ -129,43 +181,7 @@ k_token_block(const T* __restrict__ x, const T* __restrict__ node_w, const T* __
         for (int i = tid; i < D; i += kTBThreads) xs[i] = xt[i];
     }
     __syncthreads();
-
-    // ---- the walk
-    int64_t n = 0;
-    if (has_top) {                                      // (summed as in token_dots)
-        float sum = 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = (u * 32 + lane) * V;
-            if (k >= D) break;
-            float xv[V], wv[V];
-            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + k), xv);
-            Elem<T>::unpack(top_row[u], wv);
-#pragma unroll
-            for (int e = 0; e < V; ++e) sum = fmaf(wv[e], xv[e], sum);
-        }
-        sum = warp_sum(sum);
-        if (lane == 0) s_logit[0][warp] = sum + top_bias;
-    }
-    for (int m = 0, buf = 0; m < depth; m += kTBLevels, buf ^= 1) {
-        const int r = min(kTBLevels, depth - m);
-        if (warp < (1 << r) - 1 && !(m == 0 && ahead)) {
-            const int lev = 31 - __clz(warp + 1);
-            const int64_t row = (((int64_t)1 << (m + lev)) - 1) + (n << lev) + (warp + 1 - (1 << lev));
-            const T* rows[1] = {node_w + row * D};
-            const float bias = Elem<T>::to_float(node_b[row]);
-            float sum[1];
-            token_dots<T, 1>(rows, xs, D, vec, lane, sum);
-            if (lane == 0) s_logit[buf][warp] = sum[0] + bias;
-        }
-        __syncthreads();
-        int p = 0;
-        for (int i = 0; i < r; ++i) {
-            const int right = s_logit[buf][p] >= 0.0f ? 1 : 0;
-            p = 2 * p + 1 + right;
-            n = 2 * n + right;
-        }
-    }
+    const int64_t n = walk.leaf(node_w, node_b, xs, D, depth, vec, warp, lane, s_logit);
     if (tid == 0) {
         if (leaf_out) leaf_out[t] = (int32_t)n;
         if (leaf_out2) leaf_out2[t] = (int32_t)n;

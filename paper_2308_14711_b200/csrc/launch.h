@@ -83,6 +83,10 @@ struct Mx4Tokens {
 int mx4_most_rows(const Mx4Layer& m, int n_leaves);
 cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* perm, const void* tiles, int n_tiles,
                            int tile_rows, int32_t* counts, int n_leaves, int cap);
+// A few tokens: the walk and the leaf in one launch, a CTA per token.
+bool mx4_token_fits(const Mx4Layer& m);
+cudaError_t mx4_tokens(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const void* node_w, const void* node_b, int depth, int32_t* leaf_out,
+                       int32_t* leaf_out2, int64_t B);
 // The tail of the walk (levels > 0) as in k_leaf_warp.
 struct Mx4Tail {
     const void *node_w = nullptr, *node_b = nullptr;

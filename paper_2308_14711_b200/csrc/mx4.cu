@@ -19,6 +19,7 @@ bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p
 int access_bytes(const void* p, int cols) { return cols % 8 == 0 && aligned(p, 16) ? 16 : 2; }
 
 constexpr int kMxSmemMost = 226 * 1024;                       // shared memory of a CTA that has an SM to itself, or shares it with another
+constexpr int kMxTokenSmemMost = 100 * 1024;
 constexpr int kMxSmemPair = (227 * 1024) / 2 - 1024 - 128;
 
 MxLayout layout(const Mx4Layer& m) { return MxLayout{m.D, m.O, m.l, m.mma}; }
@@ -123,6 +124,47 @@ cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Token
     return m.big ? launch_tiles<2, true, true>(on, a, n_tiles) : launch_tiles<2, true, false>(on, a, n_tiles);
 }
 
+namespace {
+
+cudaError_t launch_token(const LaunchOn& on, void (*kern)(MxTokenArgs), int smem, const MxTokenArgs& a, int64_t B) {
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMxTokenSmemMost);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_on(on, kern, (unsigned)B, 1, kTBThreads, (size_t)smem, a);
+}
+
+template <int MT, bool kWide, bool kBig>
+cudaError_t launch_token(const LaunchOn& on, const MxTokenArgs& a, int64_t B) {
+    return launch_token(on, k_mx4_token<MT, kWide, kBig>, MxTokenSmem{a.lay.D, a.lay.Kp()}.bytes(), a, B);
+}
+
+}  // namespace
+
+bool mx4_token_fits(const Mx4Layer& m) { return MxTokenSmem{m.D, layout(m).Kp()}.bytes() <= kMxTokenSmemMost; }
+
+cudaError_t mx4_tokens(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const void* node_w, const void* node_b, int depth, int32_t* leaf_out,
+                       int32_t* leaf_out2, int64_t B) {
+    MxTokenArgs a = {};
+    a.x = (const __nv_bfloat16*)t.x;
+    a.node_w = (const __nv_bfloat16*)node_w;
+    a.node_b = (const __nv_bfloat16*)node_b;
+    a.image = m.image;
+    a.y = (__nv_bfloat16*)t.y;
+    a.leaf_out = leaf_out;
+    a.leaf_out2 = leaf_out2;
+    a.lay = layout(m);
+    a.depth = depth;
+    a.act = t.act;
+    a.x_vec = access_bytes(t.x, m.D) == 16;
+    a.y_vec = access_bytes(t.y, m.O) == 16;
+    a.big = m.big;
+    if (!m.mma) return launch_token(on, k_mx4_token_rows, MxTokenSmem{m.D, 0}.x(), a, B);
+    if (m.l <= 16) return m.big ? launch_token<1, false, true>(on, a, B) : launch_token<1, false, false>(on, a, B);
+    if (m.l <= 32) return m.big ? launch_token<2, false, true>(on, a, B) : launch_token<2, false, false>(on, a, B);
+    return m.big ? launch_token<2, true, true>(on, a, B) : launch_token<2, true, false>(on, a, B);
+}
+
 cudaError_t mx4_leaf_rows(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* leaf_idx, const int32_t* perm, int64_t B,
                           const Mx4Tail& tail) {
     MxRowsArgs a = {};
@@ -149,3 +191,4 @@ cudaError_t mx4_leaf_rows(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens
 }
 
 }  // namespace fff
+
