@@ -239,12 +239,21 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
 
 constexpr int kSlopeThreads = 512;
 
-// Tokens that count: the sum of the counts (all of which belong to such tokens).  By all threads of a CTA.
+// Tokens that count: the sum of the counts (all of which belong to such tokens).  By all threads of a CTA.  (Counts are read as vectors,
+// several in flight: one by one, four thousand took a CTA 8 us.)
 __device__ __forceinline__ double counted_tokens(const int32_t* __restrict__ counts, int n_leaves, long long* s_red) {
     const int tid = threadIdx.x;
     long long n = 0;
+    if ((reinterpret_cast<uintptr_t>(counts) & 15) == 0 && n_leaves >= 4) {
 #pragma unroll 4
-    for (int j = tid; j < n_leaves; j += blockDim.x) n += __ldg(counts + j);
+        for (int j = tid; j < n_leaves >> 2; j += blockDim.x) {
+            const int4 q = __ldg(reinterpret_cast<const int4*>(counts) + j);
+            n += (long long)q.x + q.y + (long long)q.z + q.w;
+        }
+    } else {
+#pragma unroll 4
+        for (int j = tid; j < n_leaves; j += blockDim.x) n += __ldg(counts + j);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(kFullMask, n, o);
     if ((tid & 31) == 0) s_red[tid >> 5] = n;
@@ -315,29 +324,28 @@ k_balance_slope(const int32_t* __restrict__ counts, const float* __restrict__ dl
 }
 
 constexpr int kRouteThreads = 256;
-constexpr int kRoutePerSm = 3;                // CTAs per SM
+constexpr int kRoutePerSm = 2;                // CTAs per SM
 constexpr int kRouteWarps = kRouteThreads / 32;
 constexpr int kRouteChunk = 512;              // leaves that one warp reduces at a time: four per lane and four times that, nine levels
-constexpr int kRouteMaxStagedLeaves = 4096;   // trees whose rows of gradients go through shared memory
+constexpr int kRouteMaxSlopeLeaves = 4096;    // trees whose slopes lie in shared memory
 
-// Where rows of mixture weights are at most a chunk, a warp takes rows for itself; longer ones a CTA.  Rows that one of them takes at a
-// time: where they are staged a multiple of four, so that their outputs start on a 16-byte boundary.
-__host__ __device__ inline bool route_staged(int n_leaves) { return n_leaves <= kRouteMaxStagedLeaves; }
-__host__ __device__ inline bool route_by_warps(int n_leaves) { return n_leaves <= kRouteChunk; }
-__host__ __device__ inline int route_rows(int n_leaves) {
-    if (route_by_warps(n_leaves)) return n_leaves >= kRouteChunk / 4 ? 4 : kRouteChunk / n_leaves;
-    return !route_staged(n_leaves) ? 1 : n_leaves >= 2048 ? 4 : 8;
-}
-// Floats of shared memory: gradients (of every warp's rows, or of the CTA's), sums of the chunks, slopes.
-struct RouteSmem {
-    int n_leaves;
+// Rows of up to a chunk are a warp's, as many at a time as make 512 weights; longer ones a CTA's, a chunk for every warp, several rows
+// at a time where that takes them (one where the batch is short).  (Rows of 2048 by single warps: 78 us instead of 72, 16 384 tokens.)
+struct RouteShape {
+    int n_leaves, rows;
     bool balance;
-    __host__ __device__ int out() const { return route_staged(n_leaves) ? (route_rows(n_leaves) * (n_leaves - 1) + 3) & ~3 : 0; }
-    __host__ __device__ int outs() const { return route_by_warps(n_leaves) ? kRouteWarps * out() : out(); }
-    __host__ __device__ int tops() const { return route_by_warps(n_leaves) ? 0 : 2 * route_rows(n_leaves) * (n_leaves / kRouteChunk); }
-    __host__ __device__ int slopes() const { return balance && route_staged(n_leaves) ? n_leaves : 0; }
-    __host__ __device__ size_t bytes() const { return sizeof(float) * (size_t)(outs() + ((tops() + 3) & ~3) + slopes()) + 16; }
+    __host__ __device__ bool by_warps() const { return n_leaves <= kRouteChunk; }
+    __host__ __device__ bool near_slopes() const { return n_leaves <= kRouteMaxSlopeLeaves; }
+    // Floats of shared memory: sums of the chunks (two groups' in turn), slopes.
+    __host__ __device__ int top() const { return by_warps() ? 0 : 2 * rows * (n_leaves / kRouteChunk); }
+    __host__ __device__ int slopes() const { return balance && near_slopes() ? n_leaves : 0; }
+    __host__ __device__ size_t bytes() const { return sizeof(float) * (size_t)(2 * top() + slopes()); }
 };
+__host__ inline RouteShape route_shape(int64_t B, int n_leaves, bool balance, int sms) {
+    if (n_leaves <= kRouteChunk) return {n_leaves, kRouteChunk / n_leaves, balance};
+    const int rows = kRouteWarps * kRouteChunk / n_leaves;
+    return {n_leaves, rows < 1 || B < (int64_t)sms * rows ? 1 : rows, balance};
+}
 
 // One node: sums over its two children's leaves in, its own out.  Children too small for float32 have no say.
 __device__ __forceinline__ float node_gradient(float ml, float sl, float mr, float sr, float& m, float& s) {
@@ -348,216 +356,243 @@ __device__ __forceinline__ float node_gradient(float ml, float sl, float mr, flo
     return m < FLT_MIN ? 0.0f : g;
 }
 
-// Up to 512 mixture weights (whole rows, or a part of one), `base` on from the first row of a group of rows that ends at `elems`: the
-// gradients of all their nodes to out (rows dense); mm, ss: the sums over a part of a row.  By one warp: every lane has four neighbouring
-// leaves of each of four chunks of 128, two levels in its registers; then up to five across the lanes, the chunks shared out on the way:
-// after the first step a lane goes on with two of the four, after the second with one, so that a level costs what its nodes do (every
-// lane going on with all four: 20 nodes and 40 shuffles instead of 6 and 12); then up to two across the chunks.
-template <bool kUp, bool kBal>
-__device__ __forceinline__ void route_chunk(const float* __restrict__ gm, const float* __restrict__ gd, const int32_t* __restrict__ leaf_idx,
-                                            const uint8_t* __restrict__ mask, const float* slopes, int64_t row0, int base, int elems, int depth,
-                                            float* out, int lane, float& mm, float& ss)
+// A lane's part of up to 512 mixture weights and what belongs to them: four neighbouring leaves of each of four chunks of 128.  D is the
+// depth, 9 for every one from 9 on (512 weights are then a row's, or a part of one's): with it known, indices are constants but for the
+// lane, and the kernel, which issue bounds, has 40 % fewer instructions.
+constexpr int kRouteU = 4;
+constexpr int kRouteDeepest = 9;
+template <int D>
+struct RouteIn {
+    static constexpr int kRows = D >= 9 ? 1 : D == 8 ? 2 : kRouteU;      // rows that the four chunks are of
+    static constexpr int row_of(int i) { return i * kRows / kRouteU; }
+    float m[kRouteU][4], g[kRouteU][4];
+    int leaf[kRows], kept[kRows];                          // of the lane's rows (not at depth 1)
+};
+
+// Loads them: `base` on from row row0, whose group of rows ends at `elems`.  What lies behind the end is some of the last row instead
+// (loads without branches; nothing of it is stored).
+template <bool kUp, bool kBal, int D>
+__device__ __forceinline__ void route_load(const float* __restrict__ mix, const float* __restrict__ dmix, const int32_t* __restrict__ leaf_idx,
+                                           const uint8_t* __restrict__ mask, int64_t row0, int base, int elems, int depth, int lane, RouteIn<D>& in)
 {
-    constexpr int U = 4;
-    const int L = 1 << depth, N = L - 1;
-    float m4[U][4], g4[U][4];
-    int leaf[U], kept[U];                                  // of the lane's row (depth >= 2)
+    const float* gm = mix + (row0 << depth);
+    const float* gd = kUp ? dmix + (row0 << depth) : nullptr;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int e = base + i * 128 + lane * 4;
+    for (int i = 0; i < kRouteU; ++i) {
+        int e = base + i * 128 + lane * 4;
+        if constexpr (D == 1) {                            // (a lane's four weights are two rows, and the last lane may have one)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { m4[i][k] = 0.0f; g4[i][k] = 0.0f; }
-        leaf[i] = 0;
-        kept[i] = 1;
-        if (e >= elems) continue;
-        if (kBal && leaf_idx) leaf[i] = __ldg(leaf_idx + row0 + (e >> depth));
-        if (mask) kept[i] = __ldg(mask + row0 + (e >> depth));
-        // (L = 2: a lane's four weights are two rows, and the last lane may have one)
-        if (depth >= 2 || e + 4 <= elems) {
+            for (int k = 0; k < 4; ++k) {
+                in.m[i][k] = e + k < elems ? gm[e + k] : 0.0f;
+                in.g[i][k] = kUp && e + k < elems ? gd[e + k] : 0.0f;
+            }
+        } else {
+            if constexpr (D < 9) e = min(e, elems - 4);
+            if (i == 0 || in.row_of(i) != in.row_of(i - 1)) {
+                const int64_t b = row0 + (e >> depth);
+                in.leaf[in.row_of(i)] = kBal && leaf_idx ? __ldg(leaf_idx + b) : 0;
+                in.kept[in.row_of(i)] = mask ? __ldg(mask + b) : 1;
+            }
             const float4 q = __ldcs(reinterpret_cast<const float4*>(gm + e));
-            m4[i][0] = q.x; m4[i][1] = q.y; m4[i][2] = q.z; m4[i][3] = q.w;
-            if constexpr (kUp) {
-                const float4 d = __ldcs(reinterpret_cast<const float4*>(gd + e));
-                g4[i][0] = d.x; g4[i][1] = d.y; g4[i][2] = d.z; g4[i][3] = d.w;
-            }
-        } else {
-            for (int k = 0; k < 2; ++k) {
-                m4[i][k] = gm[e + k];
-                if constexpr (kUp) g4[i][k] = gd[e + k];
-            }
+            in.m[i][0] = q.x; in.m[i][1] = q.y; in.m[i][2] = q.z; in.m[i][3] = q.w;
+            const float4 d = kUp ? __ldcs(reinterpret_cast<const float4*>(gd + e)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            in.g[i][0] = d.x; in.g[i][1] = d.y; in.g[i][2] = d.z; in.g[i][3] = d.w;
         }
     }
-    if (kBal || mask) {
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int e = base + i * 128 + lane * 4;
-            if (e >= elems) continue;
-            if (depth >= 2) {
-                if (kBal && (unsigned)leaf[i] < (unsigned)L) {
-                    const float4 q = *reinterpret_cast<const float4*>(slopes + (e & (L - 1)));
-                    g4[i][0] += q.x; g4[i][1] += q.y; g4[i][2] += q.z; g4[i][3] += q.w;
-                }
-                if (!kept[i]) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) m4[i][k] = g4[i][k] = 0.0f;
-                }
-                continue;
-            }
-#pragma unroll
-            for (int k = 0; k < 4; k += 2) {               // (L = 2: two rows)
-                if (e + k >= elems) break;
-                const int64_t b = row0 + ((e + k) >> 1);
-                if (kBal && (!leaf_idx || (unsigned)__ldg(leaf_idx + b) < 2u)) {
-                    g4[i][k] += slopes[0];
-                    g4[i][k + 1] += slopes[1];
-                }
-                if (mask && __ldg(mask + b) == 0) m4[i][k] = m4[i][k + 1] = g4[i][k] = g4[i][k + 1] = 0.0f;
-            }
-        }
-    }
-    float m[U], t[U];                                      // sums over the lane's four leaves
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int e = base + i * 128 + lane * 4, row = e >> depth, j = e & (L - 1);
-        float ma, sa, mb, sb;
-        const float (&w)[4] = m4[i];
-        const float g0 = node_gradient(w[0], w[0] * g4[i][0], w[1], w[1] * g4[i][1], ma, sa);
-        const float g1 = node_gradient(w[2], w[2] * g4[i][2], w[3], w[3] * g4[i][3], mb, sb);
-        const float g2 = node_gradient(ma, sa, mb, sb, m[i], t[i]);
-        if (e >= elems) continue;
-        if (depth == 1) {
-            out[row] = g0;
-            if (e + 2 < elems) out[row + 1] = g1;
-        } else {
-            float* o = out + row * N;
-            const int last = (1 << (depth - 1)) - 1 + (j >> 1);          // first of two nodes above the leaves
-            o[last] = g0;
-            o[last + 1] = g1;
-            o[(1 << (depth - 2)) - 1 + (j >> 2)] = g2;
-        }
-    }
-    // the node 2^(2 + k) leaves wide that leaf `at` of the chunk belongs to
-    auto store = [&](int at, int k, float g) {
-        const int e = base + at;
-        if (e < elems) out[(e >> depth) * N + (1 << (depth - 2 - k)) - 1 + ((e & (L - 1)) >> (2 + k))] = g;
-    };
-    const bool r0 = lane & 1, r1 = lane & 2;
-    mm = ss = 0.0f;
-    if (depth < 3) return;
-    float m2[2], t2[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        // chunk i stays with even lanes, chunk 2 + i with odd ones
-        const float mo = __shfl_xor_sync(kFullMask, r0 ? m[i] : m[2 + i], 1), to = __shfl_xor_sync(kFullMask, r0 ? t[i] : t[2 + i], 1);
-        const float mk = r0 ? m[2 + i] : m[i], tk = r0 ? t[2 + i] : t[i];
-        const float g = node_gradient(r0 ? mo : mk, r0 ? to : tk, r0 ? mk : mo, r0 ? tk : to, m2[i], t2[i]);
-        store((r0 ? 2 + i : i) * 128 + (lane & ~1) * 4, 1, g);
-    }
-    if (depth < 4) return;
-    const int mine = ((r0 ? 2 : 0) + (r1 ? 1 : 0)) * 128;  // first leaf of the chunk that the lane goes on with
-    auto up = [&](int lanes, bool right) {                 // one more level: with the lane that has the other child
-        const float mo = __shfl_xor_sync(kFullMask, mm, lanes), so = __shfl_xor_sync(kFullMask, ss, lanes);
-        return node_gradient(right ? mo : mm, right ? so : ss, right ? mm : mo, right ? ss : so, mm, ss);
-    };
-    {
-        const float mo = __shfl_xor_sync(kFullMask, r1 ? m2[0] : m2[1], 2), to = __shfl_xor_sync(kFullMask, r1 ? t2[0] : t2[1], 2);
-        const float mk = r1 ? m2[1] : m2[0], tk = r1 ? t2[1] : t2[0];
-        const float g = node_gradient(r1 ? mo : mk, r1 ? to : tk, r1 ? mk : mo, r1 ? tk : to, mm, ss);
-        store(mine + (lane & ~3) * 4, 2, g);
-    }
-#pragma unroll
-    for (int k = 3; k <= 5; ++k) {
-        if (k > depth - 2) return;
-        const float g = up(1 << (k - 1), (lane >> (k - 1)) & 1);
-        if (((lane >> 2) & ((1 << (k - 2)) - 1)) == 0) store(mine + (lane & ~((1 << k) - 1)) * 4, k, g);
-    }
-    // chunks 0 and 1, 2 and 3; then both pairs
-    if (depth < 8) return;
-    float g = up(2, r1);
-    if ((lane & ~1) == 0) store(mine, 6, g);
-    if (depth < 9) return;
-    g = up(1, r0);
-    if (lane == 0) store(mine, 7, g);
 }
 
-// n floats from shared to global memory (both on 16-byte boundaries), by `threads` threads.
-__device__ __forceinline__ void route_copy(float* __restrict__ dst, const float* src, int n, int id, int threads) {
-    for (int i = id; i < n >> 2; i += threads) __stcs(reinterpret_cast<float4*>(dst) + i, reinterpret_cast<const float4*>(src)[i]);
-    for (int i = (n & ~3) + id; i < n; i += threads) dst[i] = src[i];
+// Where the gradients of such weights go: to rows from `out` on, dense.
+template <int D>
+struct RouteOut {
+    float* out;                                            // D = 9: the row
+    int depth, at, elems;                                  // weights: first (D = 9: of the row), how many
+    // the node 2^(2 + k) leaves wide that leaf w of them belongs to (k = -1: the first of two)
+    __device__ __forceinline__ float* node(int w, int k) const {
+        if constexpr (D >= 9) return out + ((1 << (depth - 2 - k)) - 1 + (at >> (2 + k))) + (w >> (2 + k));
+        else return out + (w >> D) * ((1 << D) - 1) + (1 << (D - 2 - k)) - 1 + ((w & ((1 << D) - 1)) >> (2 + k));
+    }
+    __device__ __forceinline__ void store(int w, int k, float g) const {
+        if (D >= 9 || w < elems) *node(w, k) = g;
+    }
+};
+
+// Two levels, in a lane's registers; m, t: the sums over its four leaves of every chunk.  slope: of the lane's leaves (D <= 7: the same
+// ones in every chunk), else slopes has them.  A row that the mask leaves out has weights of zero, which give zeros whatever its
+// gradients are.
+template <bool kBal, int D>
+__device__ __forceinline__ void route_low(RouteIn<D>& in, const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask,
+                                          const float* slopes, float4 slope, int64_t row0, const RouteOut<D>& to, int lane,
+                                          float (&m)[kRouteU], float (&t)[kRouteU])
+{
+    const int L = D >= 9 ? 1 << to.depth : 1 << D;
+#pragma unroll
+    for (int i = 0; i < kRouteU; ++i) {
+        const int e = i * 128 + lane * 4;
+        float (&w)[4] = in.m[i], (&d)[4] = in.g[i];
+        if constexpr (D == 1) {
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {
+                if (e + k >= to.elems) break;
+                const int64_t b = row0 + ((e + k) >> 1);
+                if (kBal && (!leaf_idx || (unsigned)__ldg(leaf_idx + b) < 2u)) { d[k] += slope.x; d[k + 1] += slope.y; }
+                if (mask && __ldg(mask + b) == 0) w[k] = w[k + 1] = 0.0f;
+            }
+        } else {
+            if (kBal && (unsigned)in.leaf[in.row_of(i)] < (unsigned)L) {
+                const float4 q = D <= 7 ? slope : *reinterpret_cast<const float4*>(slopes + (D == 8 ? e & 255 : to.at + e));
+                d[0] += q.x; d[1] += q.y; d[2] += q.z; d[3] += q.w;
+            }
+            if (!in.kept[in.row_of(i)]) w[0] = w[1] = w[2] = w[3] = 0.0f;
+        }
+        float ma, sa, mb, sb;
+        const float g0 = node_gradient(w[0], w[0] * d[0], w[1], w[1] * d[1], ma, sa);
+        const float g1 = node_gradient(w[2], w[2] * d[2], w[3], w[3] * d[3], mb, sb);
+        if constexpr (D == 1) {
+            if (e < to.elems) to.out[e >> 1] = g0;
+            if (e + 2 < to.elems) to.out[(e >> 1) + 1] = g1;
+        } else {
+            const float g2 = node_gradient(ma, sa, mb, sb, m[i], t[i]);
+            if (D >= 9 || e < to.elems) {
+                float* last = to.node(e, -1);
+                last[0] = g0;
+                last[1] = g1;
+                *to.node(e, 0) = g2;
+            }
+        }
+    }
+}
+
+// The levels above: up to five across the lanes, the chunks shared out on the way: after the first step a lane goes on with two of the
+// four, after the second with one, so that a level costs what its nodes do (every lane going on with all four: 20 nodes and 40 shuffles
+// instead of 6 and 12); then up to two across the chunks.  mm, ss: the sums over all 512.
+template <int D>
+__device__ __forceinline__ void route_high(const float (&m)[kRouteU], const float (&t)[kRouteU], const RouteOut<D>& to, int lane, float& mm, float& ss)
+{
+    const bool r0 = lane & 1, r1 = lane & 2;
+    mm = ss = 0.0f;
+    if constexpr (D >= 3) {
+        float m2[2], t2[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            // chunk i stays with even lanes, chunk 2 + i with odd ones
+            const float mo = __shfl_xor_sync(kFullMask, r0 ? m[i] : m[2 + i], 1), so = __shfl_xor_sync(kFullMask, r0 ? t[i] : t[2 + i], 1);
+            const float mk = r0 ? m[2 + i] : m[i], sk = r0 ? t[2 + i] : t[i];
+            const float g = node_gradient(r0 ? mo : mk, r0 ? so : sk, r0 ? mk : mo, r0 ? sk : so, m2[i], t2[i]);
+            to.store((lane & 1) * 256 + i * 128 + (lane & ~1) * 4, 1, g);
+        }
+        if constexpr (D >= 4) {
+            const int mine = (lane & 1) * 256 + (lane & 2) * 64;         // first leaf of the chunk that the lane goes on with
+            {
+                const float mo = __shfl_xor_sync(kFullMask, r1 ? m2[0] : m2[1], 2), so = __shfl_xor_sync(kFullMask, r1 ? t2[0] : t2[1], 2);
+                const float mk = r1 ? m2[1] : m2[0], sk = r1 ? t2[1] : t2[0];
+                const float g = node_gradient(r1 ? mo : mk, r1 ? so : sk, r1 ? mk : mo, r1 ? sk : so, mm, ss);
+                to.store(mine + (lane & ~3) * 4, 2, g);
+            }
+            auto up = [&](int lanes, bool right) {         // one more level: with the lane that has the other child
+                const float mo = __shfl_xor_sync(kFullMask, mm, lanes), so = __shfl_xor_sync(kFullMask, ss, lanes);
+                return node_gradient(right ? mo : mm, right ? so : ss, right ? mm : mo, right ? ss : so, mm, ss);
+            };
+#pragma unroll
+            for (int k = 3; k <= 5; ++k) {
+                if (k > D - 2) break;
+                const float g = up(1 << (k - 1), (lane >> (k - 1)) & 1);
+                if (((lane >> 2) & ((1 << (k - 2)) - 1)) == 0) to.store(mine + (lane & ~((1 << k) - 1)) * 4, k, g);
+            }
+            // chunks 0 and 1, 2 and 3; then both pairs
+            if constexpr (D >= 8) {
+                const float g = up(2, r1);
+                if ((lane & ~1) == 0) to.store(mine, 6, g);
+            }
+            if constexpr (D >= 9) {
+                const float g = up(1, r0);
+                if (lane == 0) to.store(0, 7, g);
+            }
+        }
+    }
 }
 
 // kUp: dmixture given; kBal: counts and dloss given (slope_table for more than kRouteMaxStagedLeaves leaves).
-// Rows of gradients are collected in shared memory and leave as aligned 16-byte vectors (a row has 2^d - 1 of them, so rows start
-// anywhere).  Rows with a zero mask give zeros.
-template <bool kUp, bool kBal>
+// Gradients are stored as they come: a row has 2^d - 1 of them and starts anywhere, a level's are next to each other, L2 puts them
+// together.  (Collected in shared memory, and stored as aligned vectors: the same times, 5 % more at 2048 leaves.)
+template <bool kUp, bool kBal, int D>
 __global__ void __launch_bounds__(kRouteThreads, kRoutePerSm)
 k_routing_backward(const float* __restrict__ mix, const float* __restrict__ dmix, const int32_t* __restrict__ leaf_idx,
                    const uint8_t* __restrict__ mask, const int32_t* __restrict__ counts, const float* __restrict__ dloss,
-                   const float* __restrict__ slope_table, float* __restrict__ dz, int64_t B, int depth)
+                   const float* __restrict__ slope_table, float* __restrict__ dz, int64_t B, int any_depth, const RouteShape S)
 {
     extern __shared__ __align__(16) float s_route[];
     __shared__ long long s_red[kRouteWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int L = 1 << depth, N = L - 1, R = route_rows(L);
-    const bool staged = route_staged(L), by_warps = route_by_warps(L);
-    const RouteSmem S{L, kBal};
-    float* s_out = s_route + (by_warps ? warp * S.out() : 0);            // [R][N]
-    float* s_top = s_route + S.outs();                                   // [2][R][chunks of a row]
-    float* s_slope = s_top + ((S.tops() + 3) & ~3);                      // [L]
-    const float* slopes = staged ? s_slope : slope_table;
+    const int depth = D < kRouteDeepest ? D : any_depth, L = 1 << depth, N = L - 1, R = S.rows, chunks = L / kRouteChunk;
+    const bool by_warps = D < kRouteDeepest || chunks == 1;
+    float* s_slope = s_route;                                            // [L]
+    float* s_top = s_route + S.slopes();                                 // [2 groups][2][R][chunks]
+    const float* slopes = S.near_slopes() ? s_slope : slope_table;
     pdl_trigger();
     pdl_wait();
-    if (kBal && staged) {
+    const int64_t groups = (B + R - 1) / R;
+    int64_t grp = by_warps ? (int64_t)blockIdx.x + (int64_t)gridDim.x * warp : blockIdx.x;
+    const int64_t stride = by_warps ? (int64_t)gridDim.x * kRouteWarps : gridDim.x;
+    const int from = by_warps ? 0 : warp, step = by_warps ? 1 : kRouteWarps;
+    auto elems_of = [&](int64_t group) { return (int)min((int64_t)R, B - group * R) * L; };
+    // a warp's next 512 weights are on their way while it works on the upper levels of these
+    RouteIn<D> in;
+    auto load = [&](int64_t group, int u) {
+        if (group < groups && u * kRouteChunk < elems_of(group))         // (a short row has none for some warps)
+            route_load<kUp, kBal, D>(mix, dmix, leaf_idx, mask, group * R, u * kRouteChunk, elems_of(group), depth, lane, in);
+    };
+    load(grp, from);
+    float4 slope = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (kBal && S.near_slopes()) {
         const double n = counted_tokens(counts, L, s_red), g = slope_scale(dloss, n);
+#pragma unroll 4
         for (int j = tid; j < L; j += kRouteThreads) s_slope[j] = centred_slope(__ldg(counts + j), L, n, g);
         __syncthreads();
-    }
-    const int64_t groups = (B + R - 1) / R;
-    float mm, ss;
-    if (by_warps) {
-        for (int64_t grp = (int64_t)blockIdx.x + (int64_t)gridDim.x * warp; grp < groups; grp += (int64_t)gridDim.x * kRouteWarps) {
-            const int64_t row0 = grp * R;
-            const int rows = (int)min((int64_t)R, B - row0), elems = rows * L;
-            for (int base = 0; base < elems; base += kRouteChunk)
-                route_chunk<kUp, kBal>(mix + row0 * L, kUp ? dmix + row0 * L : nullptr, leaf_idx, mask, slopes, row0, base, elems, depth, s_out, lane, mm, ss);
-            __syncwarp();
-            route_copy(dz + row0 * N, s_out, rows * N, lane, 32);
-            __syncwarp();
+        if constexpr (D <= 7) {
+            const float* at = s_slope + (lane * 4 & (L - 1));
+            slope = D == 1 ? make_float4(at[0], at[1], 0.0f, 0.0f) : *reinterpret_cast<const float4*>(at);
         }
-        return;
     }
-    const int chunks = L / kRouteChunk;
-    for (int64_t grp = blockIdx.x; grp < groups; grp += gridDim.x) {
+    for (int turn = 0; grp < groups; grp += stride, turn ^= 1) {
         const int64_t row0 = grp * R;
-        const int rows = (int)min((int64_t)R, B - row0), elems = rows * L;
-        float* out = staged ? s_out : dz + row0 * N;
-        for (int u = warp; u < rows * chunks; u += kRouteWarps) {
-            route_chunk<kUp, kBal>(mix + row0 * L, kUp ? dmix + row0 * L : nullptr, leaf_idx, mask, slopes, row0, u * kRouteChunk, elems, depth, out, lane, mm, ss);
-            if (lane == 0) {
-                s_top[u] = mm;                                           // u = row * chunks + chunk
-                s_top[R * chunks + u] = ss;
+        const int elems = elems_of(grp), rows = elems >> depth;
+        float* out = dz + row0 * N;
+        float* top = s_top + turn * S.top();
+        for (int u = from; u * kRouteChunk < elems; u += step) {
+            const int base = u * kRouteChunk;
+            RouteOut<D> nodes{out, depth, 0, elems};
+            if constexpr (D >= kRouteDeepest) {
+                nodes.out = out + (int64_t)(base >> depth) * N;
+                nodes.at = base & (L - 1);
+            }
+            float m[kRouteU], t[kRouteU], mm, ss;
+            route_low<kBal, D>(in, leaf_idx, mask, slopes, slope, row0, nodes, lane, m, t);
+            const bool more = (u + step) * kRouteChunk < elems;
+            load(more ? grp : grp + stride, more ? u + step : from);
+            route_high<D>(m, t, nodes, lane, mm, ss);
+            if (!by_warps && lane == 0) {
+                top[u] = mm;                                             // u = row * chunks + chunk
+                top[R * chunks + u] = ss;
             }
         }
-        // the levels above the chunks: a warp per row, in place (a step's reads lie ahead of its writes)
+        if (by_warps) continue;
+        // The levels above the chunks: a warp per row, in place (a step's reads lie ahead of its writes).  One barrier per group: the other
+        // warps go on to the next, whose sums have another place.
         __syncthreads();
         for (int row = warp; row < rows; row += kRouteWarps) {
-            float* tm = s_top + row * chunks;
+            float* tm = top + row * chunks;
             float* ts = tm + R * chunks;
             float* o = out + (int64_t)row * N;
             for (int nodes = chunks >> 1; nodes >= 1; nodes >>= 1) {
                 for (int p0 = 0; p0 < nodes; p0 += 32) {
                     const int p = p0 + lane;
+                    float mm, ss;
                     if (p < nodes) o[nodes - 1 + p] = node_gradient(tm[2 * p], ts[2 * p], tm[2 * p + 1], ts[2 * p + 1], mm, ss);
                     __syncwarp();
                     if (p < nodes) { tm[p] = mm; ts[p] = ss; }
                     __syncwarp();
                 }
             }
-        }
-        __syncthreads();
-        if (staged) {
-            route_copy(dz + row0 * N, s_out, rows * N, tid, kRouteThreads);
-            __syncthreads();
         }
     }
 }

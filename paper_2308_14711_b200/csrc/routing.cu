@@ -2,15 +2,13 @@
 #include "kernels/routing.cuh"
 
 #include <algorithm>
-#include <mutex>
+#include <type_traits>
 
 #include "launch.h"
 
 namespace fff {
 
 namespace {
-
-constexpr int kMaxDevices = 64;
 
 int balance_tiles(int64_t n_leaves) { return (int)std::max<int64_t>(1, n_leaves / kBalCols); }
 
@@ -67,31 +65,34 @@ cudaError_t routing_backward(const LaunchOn& on, const float* mixture, const flo
     const int L = 1 << depth;
     const bool up = dmixture != nullptr, bal = counts != nullptr;
     *launches = 0;
-    if (bal && !route_staged(L)) {
+    const RouteShape shape = route_shape(B, L, bal, on.sm_count);
+    if (bal && !shape.near_slopes()) {
         const cudaError_t e = launch_on(on, k_balance_slope, (unsigned)std::min(on.sm_count, L / 1024), 1, 1024, 0, counts, dloss, slope, L);
         if (e != cudaSuccess) return e;
         ++*launches;
     }
-    const auto kern = up ? (bal ? k_routing_backward<true, true> : k_routing_backward<true, false>) : k_routing_backward<false, true>;
-    const size_t smem = RouteSmem{L, bal}.bytes();
-    const int which = up ? (bal ? 0 : 1) : 2;
-    if (smem > 48 * 1024) {
-        static std::mutex mu;
-        static bool raised[3][kMaxDevices] = {};
-        std::lock_guard<std::mutex> lk(mu);
-        if (!raised[which][on.device]) {
-            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-            if (e != cudaSuccess) return e;
-            raised[which][on.device] = true;
-        }
-    }
-    const int64_t groups = (B + route_rows(L) - 1) / route_rows(L);
-    const int per_sm = (int)std::max<size_t>(1, std::min<size_t>(kRoutePerSm, (size_t)(227 * 1024) / (smem + 1024)));
-    const int64_t ctas = route_by_warps(L) ? (groups + kRouteWarps - 1) / kRouteWarps : groups;
+    const int64_t groups = (B + shape.rows - 1) / shape.rows;
+    const int64_t ctas = shape.by_warps() ? (groups + kRouteWarps - 1) / kRouteWarps : groups;
     // (a batch that would not give every SM a CTA: a warp of work each)
-    const unsigned grid = (unsigned)std::min<int64_t>(ctas < on.sm_count ? groups : ctas, (int64_t)on.sm_count * per_sm);
-    const cudaError_t e = launch_on(on, kern, grid, 1, kRouteThreads, smem, mixture, dmixture, leaf_idx, mask, counts, dloss,
-                                    (const float*)slope, dlogits, B, depth);
+    const unsigned grid = (unsigned)std::min<int64_t>(ctas < on.sm_count ? groups : ctas, (int64_t)on.sm_count * kRoutePerSm);
+    const auto launch = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        const auto kern = up ? (bal ? k_routing_backward<true, true, D> : k_routing_backward<true, false, D>) : k_routing_backward<false, true, D>;
+        return launch_on(on, kern, grid, 1, kRouteThreads, shape.bytes(), mixture, dmixture, leaf_idx, mask, counts, dloss, (const float*)slope,
+                         dlogits, B, depth, shape);
+    };
+    cudaError_t e;
+    switch (std::min(depth, kRouteDeepest)) {
+    case 1: e = launch(std::integral_constant<int, 1>()); break;
+    case 2: e = launch(std::integral_constant<int, 2>()); break;
+    case 3: e = launch(std::integral_constant<int, 3>()); break;
+    case 4: e = launch(std::integral_constant<int, 4>()); break;
+    case 5: e = launch(std::integral_constant<int, 5>()); break;
+    case 6: e = launch(std::integral_constant<int, 6>()); break;
+    case 7: e = launch(std::integral_constant<int, 7>()); break;
+    case 8: e = launch(std::integral_constant<int, 8>()); break;
+    default: e = launch(std::integral_constant<int, kRouteDeepest>());
+    }
     if (e == cudaSuccess) ++*launches;
     return e;
 }
