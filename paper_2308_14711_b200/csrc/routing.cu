@@ -10,16 +10,16 @@ namespace fff {
 
 namespace {
 
-int balance_tiles(int64_t n_leaves) { return (int)std::max<int64_t>(1, n_leaves / kBalCols); }
+int balance_tiles(int64_t n_leaves, int cols = kBalCols) { return (int)std::max<int64_t>(1, n_leaves / cols); }
 
 // Slices so that every thread of a CTA has a few rows to add up; one where the whole batch is little more than that.
-int slices_for(int64_t B, int64_t n_leaves, int threads, int rows_each, int most) {
-    const int64_t cols = std::min<int64_t>(n_leaves, kBalCols), down = threads / (cols >= 4 ? cols / 4 : cols);
+int slices_for(int64_t B, int64_t cols, int threads, int rows_each, int most) {
+    const int64_t down = threads / (cols >= 4 ? cols / 4 : cols);
     return (int)std::max<int64_t>(1, std::min<int64_t>(most, (B + down * rows_each - 1) / (down * rows_each)));
 }
 
 BalanceScratch layout(void* scratch, int64_t n_leaves) {
-    const size_t T = balance_tiles(n_leaves), S = balance_max_slices((int)T), G = balance_groups((int)S);
+    const size_t T = balance_tiles(n_leaves), S = balance_max_slices((int)T), G = balance_groups((int)S, (int)std::min<int64_t>(n_leaves, kBalCols));
     BalanceScratch ws;
     ws.loss = static_cast<double*>(scratch);
     ws.group_sums = ws.loss + ((T + 1) & ~(size_t)1);      // (the rest starts on a 16-byte boundary)
@@ -38,23 +38,23 @@ float* balance_scratch_slope(void* scratch, int64_t n_leaves) {
 }
 
 size_t balance_scratch_bytes(int64_t n_leaves) {
-    const size_t T = balance_tiles(n_leaves), S = balance_max_slices((int)T), G = balance_groups((int)S);
+    const size_t T = balance_tiles(n_leaves), S = balance_max_slices((int)T), G = balance_groups((int)S, (int)std::min<int64_t>(n_leaves, kBalCols));
     return 8 * (T + 1) + 8 * (G * n_leaves + 1) + 8 * S * n_leaves + 4 * (G * n_leaves + S * T + G * T + T * (G + 1) + 1);
 }
 
 cudaError_t balance_loss(const LaunchOn& on, const float* mixture, const int32_t* leaf_idx, const uint8_t* mask, float* loss,
                          int32_t* counts, float* mean, int64_t B, int64_t n_leaves, void* scratch) {
-    const int S = slices_for(B, n_leaves, kBalThreads, 8, balance_max_slices(balance_tiles(n_leaves)));
+    const int S = slices_for(B, std::min<int64_t>(n_leaves, kBalCols), kBalThreads, 8, balance_max_slices(balance_tiles(n_leaves)));
     const unsigned T = (unsigned)balance_tiles(n_leaves);
-    return launch_on(on, n_leaves >= 4 ? k_balance_loss<4> : k_balance_loss<1>, (unsigned)S, T, kBalThreads, 0, mixture, leaf_idx, mask, loss,
+    return launch_on(on, n_leaves < 4 ? k_balance_loss<1, true> : n_leaves <= 32 ? k_balance_loss<4, true> : k_balance_loss<4, false>, (unsigned)S, T, kBalThreads, 0, mixture, leaf_idx, mask, loss,
                      counts, mean, B, (int)n_leaves, layout(scratch, n_leaves));
 }
 
 cudaError_t balance_loss_backward(const LaunchOn& on, const int32_t* leaf_idx, const uint8_t* mask, const int32_t* counts,
                                   const float* dloss, float* dmixture, int64_t B, int64_t n_leaves) {
-    const unsigned T = (unsigned)balance_tiles(n_leaves);
+    const unsigned T = (unsigned)balance_tiles(n_leaves, kSlopeCols);
     const int most = std::max(1, on.sm_count * 4 / (int)T);
-    const int S = slices_for(B, n_leaves, kSlopeThreads, 4, most);
+    const int S = slices_for(B, std::min<int64_t>(n_leaves, kSlopeCols), kSlopeThreads, 4, most);
     return launch_on(on, n_leaves >= 4 ? k_balance_loss_backward<4> : k_balance_loss_backward<1>, (unsigned)S, T, kSlopeThreads, 0, leaf_idx,
                      mask, counts, dloss, dmixture, B, (int)n_leaves);
 }
