@@ -52,6 +52,7 @@ struct fff_handle_s {
     int device = 0;
     int sm_count = 148;
     int D = 0, O = 0, depth = 0, l = 0;
+    int x_cols = 0;               // row length of x: D, which layers of 4-bit leaf weights round up to whole 16-byte vectors
     int Dp = 0;                   // D rounded up to the K step of the tensor-core images, which are padded with zero columns
     bool padded() const { return D != Dp; }      // the leaf kernels then keep the hidden values' float32 precision (kSplit in leaf_umma.cuh)
     int act = 0, dtype = 0;
@@ -91,6 +92,7 @@ struct fff_handle_s {
     bool ncursor_dirty = false;
     bool nslots_here = false;          // the stage being launched files its tokens under the nodes it reaches
     fff::Tile* ws_tiles = nullptr;
+    void *ws_x = nullptr, *ws_y = nullptr;      // rows of x (D) and y as whole 16-byte vectors, where the caller's are not (4-bit leaf weights)
 
     // workspace
     int64_t cap_B = 0;
@@ -307,6 +309,7 @@ void release(fff_handle_s* h) {
     dfree(h->w1codes); dfree(h->w2codes); dfree(h->scale1); dfree(h->scale2);
     dfree(h->tr_w2t); dfree(h->tr_w1t); dfree(h->tr_b1t); dfree(h->tr_wn); dfree(h->tr_bn); dfree(h->tr_c); dfree(h->tr_mix); dfree(h->tr_entpart); dfree(h->tr_hp);
     dfree(h->w1img); dfree(h->b1img); dfree(h->w2img); dfree(h->w2uimg); dfree(h->ws_sched); dfree(h->ws_tiles); dfree(h->ws_rank); dfree(h->ws_rank8); dfree(h->ws_counts8); dfree(h->ws_blocksum); dfree(h->ws_matrix); dfree(h->ws_slots); dfree(h->ws_cursor); dfree(h->ws_nslots); dfree(h->ws_ncursor);
+    dfree(h->ws_x); dfree(h->ws_y);
     if (h->copy_in) cudaStreamDestroy(h->copy_in);
     if (h->copy_out) cudaStreamDestroy(h->copy_out);
     for (int i = 0; i < fff_handle_s::kMaxHostChunks; ++i) {
@@ -447,7 +450,8 @@ fff_status_t grow_workspace(fff_handle_s* h, int64_t B) {
     ++h->epoch;
     dfree(h->ws_leaf); dfree(h->ws_perm); dfree(h->ws_perm2); dfree(h->ws_tiles); dfree(h->ws_rank); dfree(h->ws_pos[0]);
     dfree(h->ws_rank8); dfree(h->ws_counts8); dfree(h->ws_blocksum); dfree(h->ws_slots); dfree(h->ws_cursor); dfree(h->ws_nslots);
-    dfree(h->ws_ncursor);
+    dfree(h->ws_ncursor); dfree(h->ws_x); dfree(h->ws_y);
+    h->ws_x = h->ws_y = nullptr;
     h->ws_slots = h->ws_cursor = h->ws_nslots = h->ws_ncursor = nullptr;
     h->slot_cap = 0;
     h->ws_rank8 = h->ws_counts8 = nullptr;
@@ -473,6 +477,8 @@ fff_status_t grow_workspace(fff_handle_s* h, int64_t B) {
         if ((s = dmalloc((void**)&h->ws_pos[1], sizeof(int32_t) * (size_t)B)) != FFF_OK) return s;
     }
     if ((s = dmalloc((void**)&h->ws_tiles, sizeof(fff::Tile) * max_tiles(h, B))) != FFF_OK) return s;
+    if (h->D != h->x_cols && (s = dmalloc(&h->ws_x, sizeof(uint16_t) * (size_t)B * h->D)) != FFF_OK) return s;
+    if (h->mx.mma && h->O % 8 != 0 && (s = dmalloc(&h->ws_y, sizeof(uint16_t) * (size_t)B * ((h->O + 7) & ~7))) != FFF_OK) return s;
     // direct lists: every leaf's list can take the whole batch, so their size grows with n_leaves * B; beyond
     // kMaxSlotBytes the forward keeps the bucketing kernel instead.  k_block_forward has no other way: for the layers that
     // run it the table stops growing there, and larger batches go through it in parts.
@@ -1060,7 +1066,17 @@ fff::LaunchOn launch_on_handle(const fff_handle_s* h, cudaStream_t st) {
     return fff::LaunchOn{st, h->device, h->sm_count, h->pdl && !h->prof_active};
 }
 
-// Layers with 4-bit leaf weights: thin leaves, a warp per token.
+// Layers with 4-bit leaf weights: their kernels (but for a CTA per token) and those of the descent on tensor cores take rows of x that are
+// whole 16-byte vectors, so other rows are copied to such.  us per forward, by kernels that take rows as they are and like this: 1023 -> 1024,
+// 2048 leaves of 32, 65 536 tokens 1001 and 240; 2000 tokens 138 and 64 (then a CTA per token, which reads them as they are).
+fff_status_t whole_rows(fff_handle_s* h, const void*& x, int64_t B, cudaStream_t st) {
+    if (h->D == h->x_cols) return FFF_OK;
+    if (fff::mx4_copy_rows(launch_on_handle(h, st), h->ws_x, h->D, x, h->x_cols, B) != cudaSuccess) return cudaGetLastError(), FFF_ERR_CUDA;
+    x = h->ws_x;
+    return launched(h, st, "pad_rows");
+}
+
+// Thin leaves, a warp per token.
 fff_status_t run_leaf_mx4_rows(fff_handle_s* h, const void* x, const int32_t* leaf_idx, const int32_t* perm, void* y, int64_t B,
                                cudaStream_t st, const DescentTail& tail, int32_t* leaf_out) {
     const fff::Mx4Tail walk{h->node_w, h->node_b, tail.level0, tail.levels, tail.pos, leaf_out};
@@ -1073,10 +1089,18 @@ fff_status_t run_leaf_mx4_rows(fff_handle_s* h, const void* x, const int32_t* le
 fff_status_t run_leaf_mx4(fff_handle_s* h, const void* x, const int32_t* perm, void* y, int64_t B, int tile_rows, cudaStream_t st) {
     // direct lists: perm is the table of lists, the tiles come from its counts
     int32_t* counts = h->slots_now && perm == h->ws_slots ? h->ws_cursor : nullptr;
-    if (fff::mx4_leaf_tiles(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->act, h->d_status}, perm, h->ws_tiles,
+    // rows of y that are no 16-byte vectors: to such, and a copy (1024 -> 1023, 2048 leaves of 32, 65 536 tokens: stored element by element
+    // 389 us per forward, like this 271; 767 -> 767, 16 leaves, 2000 tokens 34)
+    fff::Mx4Layer mx = h->mx;
+    const bool cut = h->O % 8 != 0;
+    mx.O = (h->O + 7) & ~7;            // (the same records)
+    if (fff::mx4_leaf_tiles(launch_on_handle(h, st), mx, fff::Mx4Tokens{x, cut ? h->ws_y : y, h->act, h->d_status}, perm, h->ws_tiles,
                             tile_list_len(B, tile_rows, (int)h->n_leaves), tile_rows, counts, (int)h->n_leaves, (int)h->slot_cap) != cudaSuccess)
         return cudaGetLastError(), FFF_ERR_CUDA;
-    return launched(h, st, "grouped_leaf_ff_mx4");
+    const fff_status_t s = launched(h, st, "grouped_leaf_ff_mx4");
+    if (s != FFF_OK || !cut) return s;
+    if (fff::mx4_copy_rows(launch_on_handle(h, st), y, h->O, h->ws_y, mx.O, B) != cudaSuccess) return cudaGetLastError(), FFF_ERR_CUDA;
+    return launched(h, st, "cut_rows");
 }
 
 // Which form of k_leaf_warp: while the warps of all tokens are resident at once with the registers that the general form wants
@@ -1555,7 +1579,7 @@ bool use_token_block(const fff_handle_s* h, int64_t B) {
 template <typename T>
 fff_status_t run_token_block(fff_handle_s* h, const void* x, void* y, int32_t* leaf_out, int32_t* leaf_out2, int64_t B, cudaStream_t st) {
     if (h->mx4) {
-        if (fff::mx4_tokens(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->act, h->d_status}, h->node_w, h->node_b, h->depth, leaf_out,
+        if (fff::mx4_tokens(launch_on_handle(h, st), h->mx, fff::Mx4Tokens{x, y, h->act, h->d_status, h->x_cols}, h->node_w, h->node_b, h->depth, leaf_out,
                             leaf_out2, B) != cudaSuccess)
             return cudaGetLastError(), FFF_ERR_CUDA;
         return launched(h, st, "forward_token_blocks_mx4");
@@ -1886,7 +1910,7 @@ namespace {
 // The images of 4-bit leaf weights, from the caller's codes and scales.
 fff_status_t make_mx4_images(fff_handle_s* h, const uint8_t* w1, const uint8_t* s1, const uint8_t* w2, const uint8_t* s2) {
     const int64_t nl = h->n_leaves, n1 = nl * h->l * ((h->D + 31) / 32), n2 = nl * h->l * ((h->O + 31) / 32);
-    h->mx.D = h->D; h->mx.O = h->O; h->mx.l = h->l;
+    h->mx.D = h->x_cols; h->mx.O = h->O; h->mx.l = h->l;
     h->mx.mma = fff::mx4_on_tensor_cores(h->l);
     if (!fff::mx4_record_fits(h->mx)) return FFF_ERR_UNSUPPORTED;
     int* flag = nullptr;
@@ -1899,6 +1923,7 @@ fff_status_t make_mx4_images(fff_handle_s* h, const uint8_t* w1, const uint8_t* 
     h->mx.big = big != 0;
     if (s == FFF_OK) s = dmalloc((void**)&h->mx.image, fff::mx4_image_bytes(h->mx, nl));
     if (s == FFF_OK && fff::mx4_pack(h->mx, w1, s1, w2, s2, h->b1, h->b2, nl, h->sm_count) != cudaSuccess) s = (cudaGetLastError(), FFF_ERR_CUDA);
+    h->mx.D = h->D;                // (the same records: their columns are padded)
     return s;
 }
 
@@ -1950,6 +1975,8 @@ fff_status_t create_common(fff_handle_t* out, int D, int O, int depth, int leaf_
         else
             cudaGetLastError();
     }
+    h->x_cols = D;
+    if (mx4) D = (D + 7) & ~7;             // (no effect on a result: the further columns of x and of the weights are zero)
     h->D = D; h->O = O; h->depth = depth; h->Dp = (D + fff::kKS - 1) / fff::kKS * fff::kKS; h->l = leaf_width; h->act = act; h->dtype = dtype;
     h->esize = dtype == FFF_DTYPE_F32 ? 4 : 2;
     h->n_nodes = ((int64_t)1 << depth) - 1;
@@ -1958,7 +1985,12 @@ fff_status_t create_common(fff_handle_t* out, int D, int O, int depth, int leaf_
 
     const size_t e = h->esize, nn = (size_t)h->n_nodes, nl = (size_t)h->n_leaves;
     fff_status_t s = FFF_OK;
-    if (s == FFF_OK) s = clone(&h->node_w, node_w, nn * D * e);
+    if (s == FFF_OK && D == h->x_cols) s = clone(&h->node_w, node_w, nn * D * e);
+    if (s == FFF_OK && D != h->x_cols && nn > 0) {
+        s = clone(&h->node_w, nullptr, nn * D * e);        // zeroed
+        if (s == FFF_OK && cudaMemcpy2D(h->node_w, D * e, node_w, h->x_cols * e, h->x_cols * e, nn, cudaMemcpyDeviceToDevice) != cudaSuccess)
+            s = (cudaGetLastError(), FFF_ERR_CUDA);
+    }
     if (s == FFF_OK) s = clone(&h->node_b, node_b, nn * e);
     h->w8 = w8;
     h->mx4 = mx4;
@@ -2104,6 +2136,7 @@ fff_status_t fff_tree_descent(fff_handle_t h, const void* x, int32_t* leaf_idx, 
     DeviceGuard g(h->device);
     if ((s = grow_workspace(h, B)) != FFF_OK) return s;
     h->launches = 0;
+    if ((s = whole_rows(h, x, B, (cudaStream_t)cuda_stream)) != FFF_OK) return s;
     return run_descent(h, x, leaf_idx, nullptr, B, (cudaStream_t)cuda_stream);
 }
 
@@ -2128,8 +2161,9 @@ fff_status_t fff_grouped_leaf_ff(fff_handle_t h, const void* x, const int32_t* l
     DeviceGuard g(h->device);
     h->launches = 0;
     cudaStream_t st = (cudaStream_t)cuda_stream;
+    if ((use_tensor_leaf(h) || h->D != h->x_cols) && (s = grow_workspace(h, B)) != FFF_OK) return s;
+    if ((s = whole_rows(h, x, B, st)) != FFF_OK) return s;
     if (use_tensor_leaf(h)) {
-        if ((s = grow_workspace(h, B)) != FFF_OK) return s;
         const LeafPlan plan = leaf_plan(h, B);
         const int tile_rows = plan.tile_rows;
         fff::k_tiles_from_offsets<<<1, fff::kBucketThreads, 0, st>>>(offsets, (int)h->n_leaves, tile_rows, h->ws_tiles,
@@ -2173,6 +2207,7 @@ fff_status_t fff_forward_infer(fff_handle_t h, const void* x, void* y, int32_t* 
         }
         return s;
     }
+    if ((s = whole_rows(h, x, B, st)) != FFF_OK) return h->prof_active = false, s;
     const bool tensor_leaf = use_tensor_leaf(h);
     // With fewer than about 4 tokens per leaf the warp leaf kernel gains nothing from bucket order (no
     // weights to share), so the bucketing is left out of the forward and made on demand
@@ -2406,7 +2441,7 @@ fff_status_t fff_forward_infer_host(fff_handle_t h, const void* x_host, void* y_
         h->pending_in_staging = false;
         dfree(h->st_x); dfree(h->st_y); dfree(h->st_leaf);
         h->st_x = h->st_y = nullptr; h->st_leaf = nullptr; h->cap_host_B = 0;
-        if ((s = dmalloc(&h->st_x, (size_t)B * h->D * h->esize)) != FFF_OK) return s;
+        if ((s = dmalloc(&h->st_x, (size_t)B * h->x_cols * h->esize)) != FFF_OK) return s;
         if ((s = dmalloc(&h->st_y, (size_t)B * h->O * h->esize)) != FFF_OK) return s;
         if ((s = dmalloc((void**)&h->st_leaf, (size_t)B * sizeof(int32_t))) != FFF_OK) return s;
         h->cap_host_B = B;
@@ -2416,7 +2451,7 @@ fff_status_t fff_forward_infer_host(fff_handle_t h, const void* x_host, void* y_
     // and the copy of chunk i-1 back overlap (tokens are independent, so chunking does not change any result).
     const int n_chunks = host_chunks(h, x_host, y_host, B);
     if (n_chunks == 1) {
-        if (cudaMemcpyAsync(h->st_x, x_host, (size_t)B * h->D * h->esize, cudaMemcpyHostToDevice, st) != cudaSuccess)
+        if (cudaMemcpyAsync(h->st_x, x_host, (size_t)B * h->x_cols * h->esize, cudaMemcpyHostToDevice, st) != cudaSuccess)
             return cudaGetLastError(), FFF_ERR_CUDA;
         if ((s = fff_forward_infer(h, h->st_x, h->st_y, h->st_leaf, B, cuda_stream)) != FFF_OK) return s;
         if (cudaMemcpyAsync(y_host, h->st_y, (size_t)B * h->O * h->esize, cudaMemcpyDeviceToHost, st) != cudaSuccess)
@@ -2439,7 +2474,7 @@ fff_status_t fff_forward_infer_host(fff_handle_t h, const void* x_host, void* y_
     }
     const int64_t chunk = (((B + n_chunks - 1) / n_chunks) + 127) & ~int64_t(127);
     const int n_full = (int)((B + chunk - 1) / chunk);
-    const size_t xrow = (size_t)h->D * h->esize, yrow = (size_t)h->O * h->esize;
+    const size_t xrow = (size_t)h->x_cols * h->esize, yrow = (size_t)h->O * h->esize;
     auto copy_leaves = [&](int64_t from, int64_t to) {
         return !leaf_idx_host || cudaMemcpyAsync(leaf_idx_host + from, h->st_leaf + from, (size_t)(to - from) * sizeof(int32_t),
                                                  cudaMemcpyDeviceToHost, h->copy_out) == cudaSuccess;
@@ -2679,7 +2714,7 @@ fff_status_t fff_stack_create(fff_stack_t* out, int n_layers, const fff_handle_t
         const fff_handle_s* h = layers[k];
         if (h->device != first->device || h->dtype != first->dtype) return FFF_ERR_INVALID_ARG;
         // a layer reads what the one before it wrote; residual connections and shared buffers need one width
-        if (h->D != first->D || h->O != first->D) return FFF_ERR_INVALID_ARG;
+        if (h->x_cols != first->x_cols || h->O != first->x_cols) return FFF_ERR_INVALID_ARG;
         for (int j = 0; j < k; ++j)
             if (layers[j] == layers[k]) return FFF_ERR_INVALID_ARG;      // a handle serves one forward at a time
     }
@@ -2687,7 +2722,7 @@ fff_status_t fff_stack_create(fff_stack_t* out, int n_layers, const fff_handle_t
     if (!s) return FFF_ERR_ALLOC;
     s->device = first->device;
     s->sm_count = first->sm_count;
-    s->D = first->D;
+    s->D = first->x_cols;
     s->dtype = first->dtype;
     s->esize = first->esize;
     s->layer_norm = layer_norm != 0;

@@ -333,7 +333,7 @@ struct MxLeafArgs {
     __nv_bfloat16* y;
     MxLayout lay;
     int act, tile_rows;                // tile_rows: a multiple of 8, at most 8 kMxMaxGroups
-    int x_bytes, y_bytes;              // widest access that rows of x and y allow, 16 or 2
+    bool y_vec;                        // rows of y are 16-byte vectors
     int* status;
 };
 
@@ -592,6 +592,63 @@ __device__ __forceinline__ int mx_bin_of_tile(const uint16_t* pre, int n_bins, i
     return lo;
 }
 
+// Rows of bf16 values from one length to another, the vectors of the leaf kernels from and to rows that start anywhere: whole vectors are
+// stored, each put together from the two of the source that it lies across, by a shift that is the same in a row.  A warp per row, of up
+// to eight vectors four rows.  Bound: HBM (65 536 rows of 1023: 64 us to whole vectors, 87 from them; floor 41).
+__global__ void __launch_bounds__(256)
+k_mx4_copy_rows(uint16_t* __restrict__ dst, int dst_cols, const uint16_t* __restrict__ src, int src_cols, int64_t rows)
+{
+    const int span = dst_cols <= 64 ? 8 : 32, lane = threadIdx.x & (span - 1), cols = min(dst_cols, src_cols), at_once = blockDim.x / span;
+    const uint16_t* end = src + rows * src_cols;
+    pdl_trigger();
+    pdl_wait();
+    for (int64_t row = (int64_t)blockIdx.x * at_once + threadIdx.x / span; row < rows; row += (int64_t)gridDim.x * at_once) {
+        const uint16_t* s = src + row * src_cols;
+        uint16_t* d = dst + row * dst_cols;
+        const int j0 = min(dst_cols, (int)(-(reinterpret_cast<uintptr_t>(d) >> 1) & 7)), vecs = (dst_cols - j0) >> 3;
+        const int sh = (int)((reinterpret_cast<uintptr_t>(s + j0) >> 1) & 7);          // elements of a vector before the first wanted
+        const bool inside = s + cols + 8 <= end;                             // no vector reaches past the buffer
+#pragma unroll 4
+        for (int i = lane; i < vecs; i += span) {
+            const int j = j0 + 8 * i;
+            const uint16_t* from = s + j - sh;                               // (on or behind the buffer's start, which is on such a boundary)
+            uint32_t w[9];
+            if (inside) {
+                // (without branches: the second vector, or the first again)
+                const uint4 a = __ldg(reinterpret_cast<const uint4*>(from));
+                const uint4 b = __ldg(reinterpret_cast<const uint4*>(sh > 0 && j + 8 - sh < cols ? from + 8 : from));
+                w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint32_t lo = from + 2 * k < end ? from[2 * k] : 0, hi = from + 2 * k + 1 < end ? from[2 * k + 1] : 0;
+                    w[k] = lo | hi << 16;
+                }
+            }
+            w[8] = 0;
+            if (sh & 4) {
+#pragma unroll
+                for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+            }
+            if (sh & 2) {
+#pragma unroll
+                for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+            }
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                o[k] = sh & 1 ? __funnelshift_r(w[k], w[k + 1], 16) : w[k];
+                const int left = cols - (j + 2 * k);                         // wanted of these two
+                o[k] = left >= 2 ? o[k] : left == 1 ? o[k] & 0xffffu : 0u;
+            }
+            *reinterpret_cast<uint4*>(d + j) = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        const int rest = j0 + 8 * vecs;
+        if (lane < j0) d[lane] = lane < cols ? s[lane] : (uint16_t)0;
+        if (lane < 8 && rest + lane < dst_cols) d[rest + lane] = rest + lane < cols ? s[rest + lane] : (uint16_t)0;
+    }
+}
+
 // A CTA per tile of up to tile_rows tokens of one leaf, two CTAs per SM.  Token rows come by bulk copies; those of the next tile are
 // sent for as soon as this tile's first product is done with the buffer, and arrive while its hidden values and outputs are computed;
 // the next leaf's record is sent for to L2 at the same time.  The first product is split along D over the warps (MT = 2: over the two
@@ -642,7 +699,6 @@ k_leaf_mx4(const MxLeafArgs A)
     const int n_tiles = A.counts ? s_pre[A.n_leaves] : A.n_tiles;
     const int units1 = Ly.units1(), at_s1 = Ly.at_s1(), at_b1 = Ly.at_b1();
     const int64_t record = Ly.record();
-    const bool bulk = A.x_bytes >= 16;
 
     // The first tile from `tile` on that is not empty (a list of tiles may contain empty ones); rows = 0: none.  Tokens `lane` and
     // `lane + 32` of it in tok.  By a whole warp.
@@ -695,7 +751,7 @@ k_leaf_mx4(const MxLeafArgs A)
         if (lane + 32 < R) s_tok2[buf * R + lane + 32] = f.tok[1];
         if (lane == 0) { s_next[buf][0] = f.tile; s_next[buf][1] = f.leaf; s_next[buf][2] = f.rows; }
         if (f.rows > 0) {
-            if (bulk) send_x(f, 0);
+            send_x(f, 0);
             if (lane == 0) mx_prefetch(A.image + f.leaf * record, record);
         }
     };
@@ -744,20 +800,18 @@ k_leaf_mx4(const MxLeafArgs A)
                 const bool fresh = unit0 == 0 || chunks > 1;           // (one chunk stays for all passes)
                 if (ch > 0 || (unit0 > 0 && chunks > 1)) {             // (the first chunk of the first pass is on its way)
                     __syncthreads();
-                    if (bulk && warp == kFinder) send_x(mine, k0);
+                    if (warp == kFinder) send_x(mine, k0);
                 }
-                if (fresh && bulk) {
+                if (fresh) {
                     if (!timed_out && !ptx::mbar_wait_suspended(&s_full, phase)) timed_out = true;
                     phase ^= 1;
-                } else if (fresh) {
-                    const int n = min(chunk, D - k0);
-                    for (int r = warp; r < rows; r += NW) {
-                        __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(xs + r * pitch);
-                        for (int k = lane; k < n; k += 32) to[k] = A.x[(int64_t)s_tok[r] * D + k0 + k];
-                        // (the last chunk's columns past D)
-                        if (chunks > 1)
-                            for (int k = n + lane; k < chunk; k += 32) to[k] = __float2bfloat16_rn(0.0f);
-                    }
+                }
+                const int past = min(chunk, (units1 - ub) * kMxUnit);      // columns that the MMAs read
+                if (chunks > 1 && k0 + past > D) {
+                    // the last chunk's columns past D hold an earlier chunk's, which zero codes do not undo where they are infinite
+                    for (int r = warp; r < rows; r += NW)
+                        for (int k = D - k0 + lane; k < past; k += 32) reinterpret_cast<__nv_bfloat16*>(xs + r * pitch)[k] = __float2bfloat16_rn(0.0f);
+                    ptx::fence_proxy_async();              // (the next copies write there)
                     __syncthreads();
                 }
                 mx_hidden<kBig, kMxMaxGroups>(rec, at_s1, l, q, xs, pitch, groups, row0, u0, u1, kSplit, ub, lane, acc);
@@ -793,7 +847,7 @@ k_leaf_mx4(const MxLeafArgs A)
         }
 
         // ---- outputs
-        mx_outputs<K16, kWide, kBig, 2>(A.y, A.y_bytes == 16, Ly, rec, hid, R, rows, s_tok, warp, NW, lane, next);
+        mx_outputs<K16, kWide, kBig, 2>(A.y, A.y_vec, Ly, rec, hid, R, rows, s_tok, warp, NW, lane, next);
         mine = following;
     }
     if (timed_out) {
@@ -822,7 +876,8 @@ struct MxTokenArgs {
     int32_t *leaf_out, *leaf_out2;     // (leaf_out2 may be nullptr)
     MxLayout lay;
     int depth, act;
-    bool x_vec, y_vec, big;            // rows of x / y are 16-byte vectors; (k_mx4_token_rows) some scale is over 2
+    int x_cols;                        // row length of x: D, or less where D is rounded up
+    bool y_vec, big;                   // rows of y are 16-byte vectors; (k_mx4_token_rows) some scale is over 2
 };
 
 // Shared memory: the token's row padded with zeros, partial sums, hidden values (eight rows of them: the operand of an MMA).
@@ -853,19 +908,19 @@ k_mx4_token(const MxTokenArgs A)
     T* hid = reinterpret_cast<T*>(smem_mt + S.x() + NW * 512);           // [2][8][Kp]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, c = lane & 3;
     TokenWalk<T> walk;
-    walk.send_first(A.node_w, A.node_b, D, A.depth, A.x_vec, warp, lane);
-    for (int i = D + tid; i < S.x() / 2; i += kTBThreads) xs[i] = __float2bfloat16_rn(0.0f);
+    walk.send_first(A.node_w, A.node_b, D, A.depth, true, warp, lane);
+    for (int i = A.x_cols + tid; i < S.x() / 2; i += kTBThreads) xs[i] = __float2bfloat16_rn(0.0f);
     if (tid < 8) s_tok[tid] = blockIdx.x;
     pdl_trigger();
     pdl_wait();
-    const T* xt = A.x + (int64_t)blockIdx.x * D;
-    if (A.x_vec) {
+    const T* xt = A.x + (int64_t)blockIdx.x * A.x_cols;
+    if (A.x_cols == D) {
         for (int i = tid; i < D / 8; i += kTBThreads) reinterpret_cast<uint4*>(xs)[i] = __ldg(reinterpret_cast<const uint4*>(xt) + i);
     } else {
-        for (int i = tid; i < D; i += kTBThreads) xs[i] = xt[i];
+        for (int i = tid; i < A.x_cols; i += kTBThreads) xs[i] = xt[i];
     }
     __syncthreads();
-    const int64_t leaf = walk.leaf(A.node_w, A.node_b, xs, D, A.depth, A.x_vec, warp, lane, s_logit);
+    const int64_t leaf = walk.leaf(A.node_w, A.node_b, xs, D, A.depth, true, warp, lane, s_logit);
     if (tid == 0) {
         A.leaf_out[blockIdx.x] = (int32_t)leaf;
         if (A.leaf_out2) A.leaf_out2[blockIdx.x] = (int32_t)leaf;
@@ -910,7 +965,7 @@ struct MxRowsArgs {
     MxLayout lay;
     int act;
     int64_t B;
-    bool x_vec, y_vec, big;            // rows of x / y are 16-byte vectors
+    bool y_vec, big;                   // rows of y are 16-byte vectors
     // the last levels of the walk, where the descent left some: from position pos[t] (0 without) of level level0
     const __nv_bfloat16 *node_w, *node_b;
     int level0, levels;
@@ -950,14 +1005,6 @@ k_leaf_mx4_rows(const MxRowsArgs A)
     const int wd = (D + 7) / 8, wo = (O + 7) / 8, nd = (int)mx_scales(D), no = (int)mx_scales(O);
     const int64_t record = Ly.record();
     float* h = s_mxh + (size_t)wib * l;
-    auto load8 = [&](const __nv_bfloat16* p, int n, bool vec, float (&v)[8]) {
-        if (vec) {
-            Elem<__nv_bfloat16>::load_vec(p, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = e < n ? __bfloat162float(p[e]) : 0.0f;
-        }
-    };
     for (int64_t i = (int64_t)blockIdx.x * kMxRowWarps + wib; i < A.B; i += (int64_t)gridDim.x * kMxRowWarps) {
         const int64_t t = A.perm ? A.perm[i] : i;
         const __nv_bfloat16* xt = A.x + t * D;
@@ -966,7 +1013,7 @@ k_leaf_mx4_rows(const MxRowsArgs A)
             int64_t n = A.pos ? A.pos[t] : 0;
             for (int m = A.level0; m < A.level0 + A.levels; ++m) {
                 const int64_t row = ((int64_t)1 << m) - 1 + n;
-                const float logit = warp_dot<__nv_bfloat16>(A.node_w + row * D, xt, D, A.x_vec, lane) + __bfloat162float(A.node_b[row]);
+                const float logit = warp_dot<__nv_bfloat16>(A.node_w + row * D, xt, D, true, lane) + __bfloat162float(A.node_b[row]);
                 n = 2 * n + (logit >= 0.0f ? 1 : 0);
             }
             j = n;
@@ -983,7 +1030,7 @@ k_leaf_mx4_rows(const MxRowsArgs A)
             float acc[U] = {};
             for (int w = lane; w < wd; w += 32) {
                 float xv[8];
-                load8(xt + 8 * w, D - 8 * w, A.x_vec, xv);
+                Elem<__nv_bfloat16>::load_vec(xt + 8 * w, xv);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     if (i0 + u >= l) break;
@@ -1003,7 +1050,7 @@ k_leaf_mx4_rows(const MxRowsArgs A)
         __nv_bfloat16* yt = A.y + t * O;
         for (int w = lane; w < wo; w += 32) {
             float acc[8];
-            load8(b2 + 8 * w, O - 8 * w, true, acc);
+            Elem<__nv_bfloat16>::load_vec(b2 + 8 * w, acc);
             for (int q = 0; q < l; ++q) {
                 float v[8];
                 mx_floats(__ldg(w2 + (int64_t)q * wo + w), __ldg(s2 + q * no + (w >> 2)), A.big, v);
@@ -1036,18 +1083,18 @@ k_mx4_token_rows(const MxTokenArgs A)
     T* xs = reinterpret_cast<T*>(smem_mt);                 // [8 wd]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     TokenWalk<T> walk;
-    walk.send_first(A.node_w, A.node_b, D, A.depth, A.x_vec, warp, lane);
-    if (tid < 8 * wd - D) xs[D + tid] = __float2bfloat16_rn(0.0f);
+    walk.send_first(A.node_w, A.node_b, D, A.depth, true, warp, lane);
+    if (tid < D - A.x_cols) xs[A.x_cols + tid] = __float2bfloat16_rn(0.0f);
     pdl_trigger();
     pdl_wait();
-    const T* xt = A.x + (int64_t)blockIdx.x * D;
-    if (A.x_vec) {
+    const T* xt = A.x + (int64_t)blockIdx.x * A.x_cols;
+    if (A.x_cols == D) {
         for (int i = tid; i < D / 8; i += kTBThreads) reinterpret_cast<uint4*>(xs)[i] = __ldg(reinterpret_cast<const uint4*>(xt) + i);
     } else {
-        for (int i = tid; i < D; i += kTBThreads) xs[i] = xt[i];
+        for (int i = tid; i < A.x_cols; i += kTBThreads) xs[i] = xt[i];
     }
     __syncthreads();
-    const int64_t leaf = walk.leaf(A.node_w, A.node_b, xs, D, A.depth, A.x_vec, warp, lane, s_logit);
+    const int64_t leaf = walk.leaf(A.node_w, A.node_b, xs, D, A.depth, true, warp, lane, s_logit);
     if (tid == 0) {
         A.leaf_out[blockIdx.x] = (int32_t)leaf;
         if (A.leaf_out2) A.leaf_out2[blockIdx.x] = (int32_t)leaf;

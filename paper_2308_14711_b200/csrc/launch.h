@@ -78,7 +78,11 @@ struct Mx4Tokens {
     void *y;
     int act;
     int* status;
+    int x_cols = 0;               // mx4_tokens: row length of x, the layer's or up to seven less
 };
+// The other kernels want rows of x that are 16-byte vectors, and store rows of y fastest that are.  Copies rows of bf16 values to rows of
+// another length (both buffers on 16-byte boundaries): what a longer row has more is zero.
+cudaError_t mx4_copy_rows(const LaunchOn& on, void* dst, int dst_cols, const void* src, int src_cols, int64_t rows);
 // Rows of the largest tile worth having; lists of up to n_leaves leaves.
 int mx4_most_rows(const Mx4Layer& m, int n_leaves);
 cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* perm, const void* tiles, int n_tiles,

@@ -15,8 +15,8 @@ std::mutex g_mu;
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// Widest access to 8 consecutive elements at a multiple of 8 in rows of `cols` bf16 values.
-int access_bytes(const void* p, int cols) { return cols % 8 == 0 && aligned(p, 16) ? 16 : 2; }
+// Whether rows of `cols` bf16 values are 16-byte vectors.
+bool whole_vectors(const void* p, int cols) { return cols % 8 == 0 && aligned(p, 16); }
 
 constexpr int kMxSmemMost = 226 * 1024;                       // shared memory of a CTA that has an SM to itself, or shares it with another
 constexpr int kMxTokenSmemMost = 100 * 1024;
@@ -101,6 +101,11 @@ int mx4_most_rows(const Mx4Layer& m, int n_leaves) {
     return 32;
 }
 
+cudaError_t mx4_copy_rows(const LaunchOn& on, void* dst, int dst_cols, const void* src, int src_cols, int64_t rows) {
+    return launch_on(on, k_mx4_copy_rows, spread(rows * (dst_cols <= 64 ? 8 : 32), 256, on.sm_count, 8), 1, 256, 0, (uint16_t*)dst, dst_cols, (const uint16_t*)src, src_cols,
+                     rows);
+}
+
 cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t, const int32_t* perm, const void* tiles, int n_tiles,
                            int tile_rows, int32_t* counts, int n_leaves, int cap) {
     MxLeafArgs a = {};
@@ -116,8 +121,7 @@ cudaError_t mx4_leaf_tiles(const LaunchOn& on, const Mx4Layer& m, const Mx4Token
     a.lay = layout(m);
     a.act = t.act;
     a.tile_rows = tile_rows;
-    a.x_bytes = access_bytes(t.x, m.D);
-    a.y_bytes = access_bytes(t.y, m.O);
+    a.y_vec = whole_vectors(t.y, m.O);
     a.status = t.status;
     if (m.l <= 16) return m.big ? launch_tiles<1, false, true>(on, a, n_tiles) : launch_tiles<1, false, false>(on, a, n_tiles);
     if (m.l <= 32) return m.big ? launch_tiles<2, false, true>(on, a, n_tiles) : launch_tiles<2, false, false>(on, a, n_tiles);
@@ -156,8 +160,8 @@ cudaError_t mx4_tokens(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens& t
     a.lay = layout(m);
     a.depth = depth;
     a.act = t.act;
-    a.x_vec = access_bytes(t.x, m.D) == 16;
-    a.y_vec = access_bytes(t.y, m.O) == 16;
+    a.x_cols = t.x_cols;
+    a.y_vec = whole_vectors(t.y, m.O);
     a.big = m.big;
     if (!m.mma) return launch_token(on, k_mx4_token_rows, MxTokenSmem{m.D, 0}.x(), a, B);
     if (m.l <= 16) return m.big ? launch_token<1, false, true>(on, a, B) : launch_token<1, false, false>(on, a, B);
@@ -176,8 +180,7 @@ cudaError_t mx4_leaf_rows(const LaunchOn& on, const Mx4Layer& m, const Mx4Tokens
     a.lay = layout(m);
     a.act = t.act;
     a.B = B;
-    a.x_vec = access_bytes(t.x, m.D) >= 16;
-    a.y_vec = access_bytes(t.y, m.O) >= 16;
+    a.y_vec = whole_vectors(t.y, m.O);
     a.big = m.big;
     a.node_w = (const __nv_bfloat16*)tail.node_w;
     a.node_b = (const __nv_bfloat16*)tail.node_b;

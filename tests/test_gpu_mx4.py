@@ -341,3 +341,96 @@ def test_conversions_that_are_refused(way, monkeypatch):
         binding.dequantize_mx4(c, s, 42)
     with pytest.raises(ValueError):
         binding.dequantize_mx4(c, s.int(), 40)
+
+
+# ---- rows that are no 16-byte vectors, and rows of several chunks
+
+ODD_CASES = [
+    C("odd_tiles", 333, 213, 6, 12, "gelu", "bf16", 3001, "normal"),
+    C("odd_in", 1021, 64, 4, 24, "relu", "bf16", 3000, "layernorm"),
+    C("odd_out", 64, 203, 3, 40, "silu", "bf16", 2500, "normal"),
+    C("even_rows", 250, 122, 5, 32, "gelu", "bf16", 2800, "normal"),       # of 4-byte words
+    C("odd_thin", 141, 77, 5, 5, "gelu", "bf16", 3000, "normal"),
+    C("few_columns", 3, 5, 2, 9, "gelu", "bf16", 5000, "normal", node_bias_std=0.5),
+    C("one_column", 1, 1, 1, 8, "relu", "bf16", 4000, "normal", node_bias_std=0.5),
+    C("odd_plain", 95, 97, 0, 33, "gelu", "bf16", 2000, "normal"),
+    C("odd_two_stages", 129, 65, 10, 16, "gelu", "bf16", 20001, "normal"),  # host buffers in chunks
+    C("chunks", 2100, 40, 3, 16, "gelu", "bf16", 1500, "normal"),          # x in three chunks, the last of 52 columns
+    C("chunks_wide", 1100, 72, 2, 70, "relu", "bf16", 1400, "normal"),
+    C("chunks_odd", 1111, 39, 3, 12, "silu", "bf16", 1500, "normal"),
+]
+
+
+@pytest.mark.parametrize("cfg", ODD_CASES, ids=lambda c: c.name)
+def test_rows_of_any_length(cfg):
+    test_forward_matches_float64(cfg)
+
+
+@pytest.mark.parametrize("l", [16, 24, 40])
+@pytest.mark.parametrize("D", [1100, 1104])
+def test_an_infinity_in_an_earlier_chunk_stays_where_it_is(D, l):
+    """Columns behind the last chunk's are nobody's: an infinite value of an earlier chunk does not turn up there (times zero: NaN)."""
+    cfg = C("inf", D, 48, 0, l, "relu", "bf16", 1500, "normal")
+    w = wl.make_weights(cfg, 3)
+    w["w1"][:, :, 100] = 1.0                               # column 100 of the second chunk is behind the end
+    w["w2"] = np.abs(w["w2"]) + 0.5
+    c1, s1 = mx.quantize(w["w1"])
+    c2, s2 = mx.quantize(np.swapaxes(w["w2"], 1, 2))
+    v1, v2 = mx.values(c1, s1), mx.values(c2, s2)
+    assert (v1[:, :, 100] > 0).all() and (v2 > 0).all()
+    layer = layer_of(cfg, w, (c1, s1), (c2, s2))
+    x = torch.from_numpy(np.random.default_rng(5).standard_normal((cfg.B, cfg.D)).astype(np.float32)).bfloat16().cuda()
+    clean, _ = layer.forward_infer(x)
+    clean = clean.clone()
+    x[7, 100] = float("inf")
+    y, _ = layer.forward_infer(x)
+    keep = torch.arange(cfg.B, device="cuda") != 7
+    assert (y[7] == float("inf")).all() and torch.equal(y[keep], clean[keep])
+    layer.close()
+
+
+@pytest.mark.parametrize("D,O,l", [(77, 51, 16), (130, 35, 9), (64, 7, 40), (61, 64, 3)])
+def test_odd_rows_keep_to_themselves(D, O, l):
+    """A NaN token stays in its row, and nothing behind the last row is written."""
+    cfg = C("rows", D, O, 2, l, "gelu", "bf16", 2500, "normal")
+    w, one, two, net, x_host = make(cfg, seed=8)
+    layer = layer_of(cfg, w, one, two)
+    x = util.to_device(x_host, "bf16")
+    clean, leaf = layer.forward_infer(x)
+    check(clean, leaf, net, cfg, w, one, two, x_host)
+    clean = clean.clone()
+    bad = [0, 17, 1003, cfg.B - 1]
+    x[bad] = float("nan")
+    flat = torch.full((cfg.B * O + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+    y = flat[:cfg.B * O].view(cfg.B, O)
+    layer.forward_infer(x, y, torch.empty(cfg.B, dtype=torch.int32, device="cuda"))
+    keep = torch.ones(cfg.B, dtype=torch.bool, device="cuda")
+    keep[bad] = False
+    assert torch.equal(y[keep], clean[keep]) and torch.isnan(y[bad]).all() and (flat[cfg.B * O:] == 7.0).all()
+    layer.close()
+
+
+def test_odd_rows_captured_and_in_a_stack():
+    cfg = C("graph", 77, 77, 5, 12, "gelu", "bf16", 2500, "normal")
+    w, one, two, net, x_host = make(cfg, seed=9)
+    layer = layer_of(cfg, w, one, two)
+    x = util.to_device(x_host, "bf16")
+    y, leaf = torch.empty((cfg.B, cfg.O), dtype=torch.bfloat16, device="cuda"), torch.empty(cfg.B, dtype=torch.int32, device="cuda")
+    layer.forward_infer(x, y, leaf)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward_infer(x, y, leaf)
+    order = np.random.default_rng(1).permutation(cfg.B)
+    y.zero_()
+    x.copy_(util.to_device(x_host[order], "bf16"))
+    graph.replay()
+    torch.cuda.synchronize()
+    check(y, leaf, net, cfg, w, one, two, x_host[order])
+    stack = FFFStack([layer, layer_of(cfg, w, one, two)], layer_norm=False, residual=False)
+    end, leaves = stack.forward(x)
+    again, last = layer.forward_infer(y.clone())
+    assert torch.equal(end, again) and torch.equal(leaves[0], leaf) and torch.equal(leaves[1], last)
+    stack.close()
+    del graph
+    layer.close()
