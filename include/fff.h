@@ -136,9 +136,10 @@ fff_status_t fff_create_w8(fff_handle_t *out, int D, int O, int depth, int leaf_
  *
  * A weight is the value of its code times 2^(scale - 127), exactly; a block with scale 255 is NaN, a product too large for bfloat16
  * infinite.  Everything else (x, y, node weights, biases) is bfloat16; products are accumulated in float32, hidden values keep
- * float32 precision to 2^-18.  (The paper stores its weights in one floating-point type; this takes 17/64 of bfloat16's bytes.)
- * Any D, O and depth; FFF_ERR_UNSUPPORTED for l > 1024.  fff_forward_train is not available on such a handle, and it stays on
- * FFF_PATH_AUTO.  The caller's arrays are read while the call runs and not kept.
+ * float32 precision to 2^-16.  (The paper stores its weights in one floating-point type; this takes 17/64 of bfloat16's bytes.)
+ * Any D, O and depth; FFF_ERR_UNSUPPORTED for l > 1024 and for leaves of 2^28 bytes and more.  Rows of x and y that are no 16-byte
+ * vectors (D % 8, O % 8) go through a workspace of B rounded-up rows, but for small batches.  fff_forward_train is not available on such a
+ * handle, and it stays on FFF_PATH_AUTO.  The caller's arrays are read while the call runs and not kept.
  */
 fff_status_t fff_create_mx4(fff_handle_t *out, int D, int O, int depth, int leaf_width, fff_activation_t act,
                             const void *node_w, const void *node_b,
@@ -221,7 +222,7 @@ fff_status_t fff_forward_train(fff_handle_t h, const void *x, void *y, float *mi
  *   counts        [2^d]     out, may be NULL: tokens of every leaf
  *   mean_mixture  [2^d]     out, may be NULL: P
  *
- * Enqueues one kernel; allocates nothing.  Sums are added in a fixed order (float32 over a few hundred tokens, float64 above).
+ * Enqueues one kernel; allocates nothing.  Sums are added in a fixed order (float32 over up to 256 tokens and over such sums of a thread, float64 above).
  * Uses scratch of the handle, like every call: one at a time.
  */
 fff_status_t fff_balance_loss(fff_handle_t h, const float *mixture, const int32_t *leaf_idx, const uint8_t *token_mask, float *loss,
@@ -421,7 +422,7 @@ fff_status_t fff_selftest_bounded_wait(fff_handle_t h, int64_t limit_cycles, voi
 typedef enum {
     FFF_CAP_TENSOR_DESCENT = 1,   /* staged descent on tensor cores (bf16, D % 128 == 0, depth > 0) */
     FFF_CAP_TCGEN05_DESCENT = 2,  /* ... its first stage on tcgen05 */
-    FFF_CAP_TENSOR_LEAF = 4,      /* grouped leaf evaluation on tensor cores (also O % 8 == 0, l <= 64) */
+    FFF_CAP_TENSOR_LEAF = 4,      /* grouped leaf evaluation on tensor cores (also O % 8 == 0, l <= 64; 4-bit leaf weights: l >= 8) */
     FFF_CAP_TCGEN05_LEAF = 8,     /* ... on tcgen05 (also O % 16 == 0) */
     FFF_CAP_FUSED_SMALL = 16,     /* FFF_PATH_FUSED may be set: small trees with thin leaves and rows that are not too wide (l <= 32;
                                      2^depth leaves of l, rounded up to a power of two, hold at most 32 neurons per SM;
@@ -433,7 +434,8 @@ typedef enum {
                                      The bits 1 to 8 then stay clear and fff_set_path refuses FFF_PATH_TENSOR, although the forward
                                      does run on tensor cores: those bits promise rows taken as they are.  Hidden values enter
                                      the second layer as sums of two bf16 values, with the float32 precision that such layers
-                                     have on CUDA cores (to 2^-18); with D % 128 == 0 they are rounded to bf16 */
+                                     have on CUDA cores (to 2^-18); with D % 128 == 0 they are rounded to bf16.  Layers with 4-bit
+                                     leaf weights have it for any other D where l >= 8 or the descent is on tensor cores */
     FFF_CAP_GROUP_TILES = 64      /* leaf tiles of 8 sibling leaves (FFF_TUNE_GROUP_TILES: 8 <= leaf_width < 16, 9 <= depth <= 11) */
 } fff_capability_t;
 int fff_capabilities(fff_handle_t h);

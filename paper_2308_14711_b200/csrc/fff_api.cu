@@ -1946,7 +1946,7 @@ fff_status_t create_common(fff_handle_t* out, int D, int O, int depth, int leaf_
     const bool w8 = w1_scale != nullptr;
     if (w8 && (!w2_scale || dtype != FFF_DTYPE_BF16)) return FFF_ERR_INVALID_ARG;
     const bool mx4 = w1_mx != nullptr, coded = w8 || mx4;
-    if (mx4 && leaf_width > fff::kMx4MaxLeafWidth) return FFF_ERR_UNSUPPORTED;
+    if (mx4 && (leaf_width > fff::kMx4MaxLeafWidth || D > 1 << 28 || O > 1 << 28)) return FFF_ERR_UNSUPPORTED;      // (mx4_record_fits; rounded up below)
     // 8-bit leaf weights run on the tcgen05 leaf kernel only
     if (w8 && (D % fff::kKS != 0 || O % 16 != 0 || leaf_width > 64 || !encode_tiled_fn())) return FFF_ERR_UNSUPPORTED;
 
@@ -2378,7 +2378,8 @@ static fff_status_t current_device(fff::LaunchOn* on, void* cuda_stream) {
 static fff_status_t check_mx4_args(fff_dtype_t dtype, int64_t rows, int64_t cols) {
     if (dtype != FFF_DTYPE_F32 && dtype != FFF_DTYPE_BF16) return FFF_ERR_INVALID_ARG;
     if (rows < 0 || cols < 0) return FFF_ERR_INVALID_ARG;
-    if (rows > 0 && cols > ((int64_t)1 << 40) / rows) return FFF_ERR_UNSUPPORTED;
+    // (the kernels number the groups of eight of a row in 32 bits)
+    if (cols > (int64_t)1 << 34 || (rows > 0 && cols > ((int64_t)1 << 40) / rows)) return FFF_ERR_UNSUPPORTED;
     return FFF_OK;
 }
 

@@ -65,3 +65,12 @@ def test_reference_by_hand():
     v = mx.values(codes, scales)[0]
     assert v[:10].tolist() == [6.0, 4.0, 2.0, 4.0, 0.0, 1.0, 1.0, -2.0, 0.0, 6.0] and v[32] == 0.25
     assert (mx.unpack(mx.pack(codes), 33) == codes).all()
+
+
+def test_rows_and_layers_too_long_for_32_bits_are_refused(lib):
+    long = (1 << 34) + 1
+    assert lib.fff_quantize_mx4(FAKE, 1, 1, long, FAKE, FAKE, None, None) == 2
+    assert lib.fff_dequantize_mx4(FAKE, FAKE, 1, 1, long, FAKE, None) == 2
+    h = C.c_void_p(1234)
+    for D, O in ((2 ** 31 - 1, 8), (8, 2 ** 31 - 1), ((1 << 28) + 1, 1)):
+        assert lib.fff_create_mx4(C.byref(h), D, O, 0, 1, 0, None, None, FAKE, FAKE, None, FAKE, FAKE, None) == 2 and h.value is None
