@@ -54,17 +54,43 @@ __device__ __forceinline__ int64_t mx_divide(int64_t unit, uint32_t d, bool smal
     return q;
 }
 
-// The values of a word's first n codes.
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// Scales in an image: a byte holds the exponent field of 2^126 2^(s - 127), which also makes up for the missing factor: s + 126, one
+// product per register.  A layer with a scale over 2 (s > 128; a block with a weight of 8 or more, or the NaN scale) keeps s itself,
+// and its kernels multiply twice (kBig).
+__device__ __forceinline__ uint32_t mx_mul1(uint32_t byte, bool big) { return (big ? min(byte, 128u) + 126u : byte) * 0x00800080u; }
+__device__ __forceinline__ uint32_t mx_mul2(uint32_t byte) {
+    return byte == 255 ? 0x7fff7fffu : (byte > 128u ? byte - 1u : 127u) * 0x00800080u;
+}
+// The values of a word's first n codes, times the scale of byte s.
 template <typename T, int kRows>
-__device__ __forceinline__ void mx_write_values(T* __restrict__ to, uint32_t word, float scale, int n) {
+__device__ __forceinline__ void mx_write_values(T* __restrict__ to, uint32_t word, int s, int n) {
+    if constexpr (kRows != kMxAny && sizeof(T) == 2) {
+        // two codes' sign, exponent and mantissa bits to a bf16's, which lacks a factor 2^126; products of powers of two, so that rounded
+        // once at most (where the value is subnormal)
+        const uint32_t f1 = mx_mul1((uint32_t)s, true), f2 = mx_mul2((uint32_t)s);
+        uint32_t o[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            const uint32_t t = word >> (8 * p) & 0xffu, x = t | t << 12;  // nibbles at bits 0 and 16
+            o[p] = mul_bf16x2((x & 0x00070007u) << 6 | (x & 0x00080008u) << 12, f1);
+        }
+        if (s > 128) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) o[p] = mul_bf16x2(o[p], f2);
+        }
+        __stcs(reinterpret_cast<uint4*>(to), make_uint4(o[0], o[1], o[2], o[3]));
+        return;
+    }
+    const float scale = mx_scale(s);
     float o[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = mx_code_value(word >> (4 * e)) * scale;
-    if constexpr (kRows != kMxAny && sizeof(T) == 2) {
-        uint4 q;
-        q.x = ptx::pack_bf16(o[0], o[1]); q.y = ptx::pack_bf16(o[2], o[3]); q.z = ptx::pack_bf16(o[4], o[5]); q.w = ptx::pack_bf16(o[6], o[7]);
-        __stcs(reinterpret_cast<uint4*>(to), q);
-    } else if constexpr (kRows != kMxAny) {
+    if constexpr (kRows != kMxAny) {
         __stcs(reinterpret_cast<float4*>(to), make_float4(o[0], o[1], o[2], o[3]));
         __stcs(reinterpret_cast<float4*>(to) + 1, make_float4(o[4], o[5], o[6], o[7]));
     } else {
@@ -112,38 +138,44 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
                 for (int e = 0; e < 8; ++e) v[u][e] = load_float(src + (e < n[u] ? at[u] + e : 0));
             }
         }
+        if constexpr (kRows == kMxAny) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if constexpr (kRows == kMxAny) {
-            } else if constexpr (sizeof(T) == 2) {
-                Elem<T>::unpack(raw[u][0], v[u]);
-            } else {
-                const uint32_t w[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w, raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[u][e] = __uint_as_float(w[e]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[u][e] = e < n[u] ? v[u][e] : 0.0f;
+                for (int e = 0; e < 8; ++e) v[u][e] = e < n[u] ? v[u][e] : 0.0f;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t unit = u0 + u * step;
-            unsigned a = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a = max(a, __float_as_uint(v[u][e]) & 0x7fffffffu);
             if (unit - (threadIdx.x & 31) >= total) break;                    // (the same answer in a whole warp)
+            unsigned a = 0;                                                   // largest magnitude, as the bits of a float32
+            if constexpr (kRows != kMxAny && sizeof(T) == 2) {
+                const uint4 w = raw[u][0];
+                Elem<T>::unpack(w, v[u]);
+                const unsigned two = __vmaxu2(__vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+                a = max(two & 0xffff0000u, two << 16);
+            } else if constexpr (kRows != kMxAny) {
+                const uint32_t w[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w, raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[u][e] = __uint_as_float(w[e]);
+                    a = max(a, w[e] & 0x7fffffffu);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a = max(a, __float_as_uint(v[u][e]) & 0x7fffffffu);
+            }
+            if (n[u] == 0) a = 0;                                             // (a group that does not exist, in a block that does)
             a = max(a, __shfl_xor_sync(kFullMask, a, 1));
             a = max(a, __shfl_xor_sync(kFullMask, a, 2));
             const int s = mx_block_scale(a);
-            const bool finite = s != 255;
             // 2^(127 - s): at most 2^127, and products of it are exact but for those far below the smallest code
-            const float inv = finite ? __uint_as_float((unsigned)(254 - s) << 23) : 0.0f;
+            const float inv = __uint_as_float((unsigned)max(254 - s, 0) << 23);
             uint32_t word = 0;
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const float2 q = finite ? make_float2(v[u][e] * inv, v[u][e + 1] * inv) : make_float2(0.0f, 0.0f);
-                word |= (uint32_t)__nv_cvt_float2_to_fp4x2(q, __NV_E2M1, cudaRoundNearest) << (4 * e);
-            }
+            for (int e = 0; e < 8; e += 2)
+                word |= (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(v[u][e] * inv, v[u][e + 1] * inv), __NV_E2M1, cudaRoundNearest) << (4 * e);
+            if (s == 255) word = 0;
             if (n[u] == 0) continue;
             if constexpr (kRows != kMxAny) {
                 *reinterpret_cast<uint32_t*>(codes + (kRows == kMxWhole ? unit * 4 : row[u] * cb + (int64_t)g[u] * 4)) = word;
@@ -152,7 +184,7 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
                 for (int e = 0; e < n[u]; e += 2) to[e >> 1] = (uint8_t)(word >> (4 * e));
             }
             if (((kRows == kMxWhole ? (uint32_t)unit : g[u]) & 3) == 0) scales[kRows == kMxWhole ? unit >> 2 : row[u] * nb + (g[u] >> 2)] = (uint8_t)s;
-            if (values) mx_write_values<T, kRows>(values + at[u], word, mx_scale(s), n[u]);
+            if (values) mx_write_values<T, kRows>(values + at[u], word, s, n[u]);
         }
     }
 }
@@ -175,7 +207,7 @@ k_dequantize_mx4(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ 
         if constexpr (kRows != kMxAny) word = __ldcs(reinterpret_cast<const uint32_t*>(codes + (kRows == kMxWhole ? unit * 4 : row * cb + (int64_t)g * 4)));
         else
             for (int e = 0; e < n; e += 2) word |= (uint32_t)codes[row * cb + (int64_t)g * 4 + (e >> 1)] << (4 * e);
-        const float sc = mx_scale(__ldg(scales + (kRows == kMxWhole ? unit >> 2 : row * nb + (g >> 2))));
+        const int sc = __ldg(scales + (kRows == kMxWhole ? unit >> 2 : row * nb + (g >> 2)));
         mx_write_values<T, kRows>(values + (kRows == kMxWhole ? unit * 8 : row * cols + (int64_t)g * 8), word, sc, n);
     }
 }
@@ -203,18 +235,6 @@ __device__ __forceinline__ void mx_expand(uint32_t w, uint32_t (&r)[4]) {
     r[1] = (w << 3) & kM;
     r[2] = (w << 6) & kM;
     r[3] = ((w << 1) & 0x80008000u) | ((w >> 5) & 0x01000100u) | ((w >> 4) & 0x00C000C0u);
-}
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
-}
-// Scales in an image: a byte holds the exponent field of 2^126 2^(s - 127), which also makes up for the missing factor: s + 126, one
-// product per register.  A layer with a scale over 2 (s > 128; a block with a weight of 8 or more, or the NaN scale) keeps s itself,
-// and its kernels multiply twice (kBig).
-__device__ __forceinline__ uint32_t mx_mul1(uint32_t byte, bool big) { return (big ? min(byte, 128u) + 126u : byte) * 0x00800080u; }
-__device__ __forceinline__ uint32_t mx_mul2(uint32_t byte) {
-    return byte == 255 ? 0x7fff7fffu : (byte > 128u ? byte - 1u : 127u) * 0x00800080u;
 }
 // The same for two codes with scales of their own (low byte of lo and of hi).
 __device__ __forceinline__ uint32_t mx_pair(uint32_t lo, uint32_t hi) { return (lo & 0xffffu) | (hi & 0xffff0000u); }

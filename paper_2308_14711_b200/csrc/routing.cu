@@ -46,7 +46,8 @@ cudaError_t balance_loss(const LaunchOn& on, const float* mixture, const int32_t
                          int32_t* counts, float* mean, int64_t B, int64_t n_leaves, void* scratch) {
     const int S = slices_for(B, std::min<int64_t>(n_leaves, kBalCols), kBalThreads, 8, balance_max_slices(balance_tiles(n_leaves)));
     const unsigned T = (unsigned)balance_tiles(n_leaves);
-    return launch_on(on, n_leaves < 4 ? k_balance_loss<1, true> : n_leaves <= 32 ? k_balance_loss<4, true> : k_balance_loss<4, false>, (unsigned)S, T, kBalThreads, 0, mixture, leaf_idx, mask, loss,
+    return launch_on(on, n_leaves < 4 ? k_balance_loss<1, kBalFew> : n_leaves <= 32 ? k_balance_loss<4, kBalFew> :
+                         n_leaves < kBalCols ? k_balance_loss<4, kBalMany> : k_balance_loss<4, kBalRows>, (unsigned)S, T, kBalThreads, 0, mixture, leaf_idx, mask, loss,
                      counts, mean, B, (int)n_leaves, layout(scratch, n_leaves));
 }
 
