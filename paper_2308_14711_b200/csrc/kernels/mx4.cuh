@@ -66,38 +66,74 @@ __device__ __forceinline__ uint32_t mx_mul1(uint32_t byte, bool big) { return (b
 __device__ __forceinline__ uint32_t mx_mul2(uint32_t byte) {
     return byte == 255 ? 0x7fff7fffu : (byte > 128u ? byte - 1u : 127u) * 0x00800080u;
 }
-// The values of a word's first n codes, times the scale of byte s.
-template <typename T, int kRows>
-__device__ __forceinline__ void mx_write_values(T* __restrict__ to, uint32_t word, int s, int n) {
-    if constexpr (kRows != kMxAny && sizeof(T) == 2) {
+// The values of a word's first n codes, times the scale of byte s.  `each`: elements that a store may have, as n and the place are
+// multiples of them: 8 or 4; or 1, and then neighbours go in pairs where they lie on an even place.
+template <typename T>
+__device__ __forceinline__ void mx_write_values(T* __restrict__ to, uint32_t word, int s, int n, int each) {
+    if constexpr (sizeof(T) == 2) {
         // two codes' sign, exponent and mantissa bits to a bf16's, which lacks a factor 2^126; products of powers of two, so that rounded
         // once at most (where the value is subnormal)
         const uint32_t f1 = mx_mul1((uint32_t)s, true), f2 = mx_mul2((uint32_t)s);
         uint32_t o[4];
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-            const uint32_t t = word >> (8 * p) & 0xffu, x = t | t << 12;  // nibbles at bits 0 and 16
+            const uint32_t t = word >> (8 * p) & 0xffu, x = t | t << 12;      // nibbles at bits 0 and 16
             o[p] = mul_bf16x2((x & 0x00070007u) << 6 | (x & 0x00080008u) << 12, f1);
         }
         if (s > 128) {
 #pragma unroll
             for (int p = 0; p < 4; ++p) o[p] = mul_bf16x2(o[p], f2);
         }
-        __stcs(reinterpret_cast<uint4*>(to), make_uint4(o[0], o[1], o[2], o[3]));
-        return;
-    }
-    const float scale = mx_scale(s);
-    float o[8];
+        if (each == 8) {
+            __stcs(reinterpret_cast<uint4*>(to), make_uint4(o[0], o[1], o[2], o[3]));
+        } else if (each == 4) {
+            if (n > 0) *reinterpret_cast<uint2*>(to) = make_uint2(o[0], o[1]);
+            if (n > 4) *reinterpret_cast<uint2*>(to + 4) = make_uint2(o[2], o[3]);
+        } else {
+            const bool odd = reinterpret_cast<uintptr_t>(to) >> 1 & 1;
+            uint16_t* one = reinterpret_cast<uint16_t*>(to);
+            if (odd && n > 0) one[0] = (uint16_t)o[0];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = mx_code_value(word >> (4 * e)) * scale;
-    if constexpr (kRows != kMxAny) {
-        __stcs(reinterpret_cast<float4*>(to), make_float4(o[0], o[1], o[2], o[3]));
-        __stcs(reinterpret_cast<float4*>(to) + 1, make_float4(o[4], o[5], o[6], o[7]));
+            for (int p = 0; p < 4; ++p) {
+                const int e = 2 * p + odd;
+                const uint32_t two = odd ? (p < 3 ? __funnelshift_r(o[p], o[p + 1], 16) : o[p] >> 16) : o[p];
+                if (e + 1 < n) *reinterpret_cast<uint32_t*>(one + e) = two;
+                else if (e < n) one[e] = (uint16_t)two;
+            }
+        }
     } else {
+        const float scale = mx_scale(s);
+        float o[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) to[e] = Elem<T>::from_float(o[e]);
+        for (int e = 0; e < 8; ++e) o[e] = mx_code_value(word >> (4 * e)) * scale;
+        if (each >= 4) {
+            if (n > 0) __stcs(reinterpret_cast<float4*>(to), make_float4(o[0], o[1], o[2], o[3]));
+            if (n > 4) __stcs(reinterpret_cast<float4*>(to) + 1, make_float4(o[4], o[5], o[6], o[7]));
+        } else {
+            const bool odd = reinterpret_cast<uintptr_t>(to) >> 2 & 1;
+            if (odd && n > 0) to[0] = o[0];
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const int e = 2 * p + odd;
+                const float a = odd ? o[2 * p + 1] : o[2 * p], b = odd ? (p < 3 ? o[2 * p + 2] : 0.0f) : o[2 * p + 1];
+                if (e + 1 < n) *reinterpret_cast<float2*>(to + e) = make_float2(a, b);
+                else if (e < n) to[e] = a;
+            }
+        }
     }
+}
+__device__ __forceinline__ int mx_store_elements(int64_t cols) { return cols % 4 == 0 ? 4 : 1; }
+
+// Eight bf16 values from value `skip` of two neighbouring 16-byte vectors on.
+__device__ __forceinline__ void mx_shift(const uint4 (&raw)[2], int skip, float (&v)[8]) {
+    uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+    for (int k = 0; k < 6; ++k) w[k] = skip & 4 ? w[k + 2] : w[k];
+#pragma unroll
+    for (int k = 0; k < 5; ++k) w[k] = skip & 2 ? w[k + 1] : w[k];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = skip & 1 ? __funnelshift_r(w[k], w[k + 1], 16) : w[k];
+    Elem<__nv_bfloat16>::unpack(make_uint4(w[0], w[1], w[2], w[3]), v);
 }
 
 // Eight elements per thread, four threads per block.  Bound: HBM.
@@ -112,11 +148,15 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
     const int64_t step = (int64_t)gridDim.x * blockDim.x;
     const bool small = total + 4 * step < ((int64_t)1 << 31);
     constexpr int U = kMxAtOnce;                           // groups whose loads are in flight
+    // A group of bf16 values that starts anywhere: from the two whole vectors that it lies across (one by one, of 16 bytes apart, 178 us
+    // instead of 113 for 65 536 rows of 999 with the pairs of mx_write_values; float32 values one by one are 8 % ahead of vectors).
+    constexpr bool kShifted = kRows == kMxAny && sizeof(T) == 2;
+    const int64_t vecs = kShifted ? rows * cols / 8 : 0;   // whole ones of the source
     // (whole warps: the shuffles below want all lanes; step is a multiple of 32, and so is the rounded total)
     const int64_t end = (total + 31) & ~(int64_t)31;
     for (int64_t u0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; u0 < end; u0 += U * step) {
         float v[U][8];
-        uint4 raw[U][sizeof(T) / 2];
+        uint4 raw[U][kShifted ? 2 : sizeof(T) / 2];
         int64_t at[U], row[U];
         uint32_t g[U];                                     // group of the row
         int n[U];                                          // elements of the group that exist
@@ -134,15 +174,31 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
                 raw[u][0] = __ldcs(from);
                 if constexpr (sizeof(T) == 4) raw[u][1] = __ldcs(from + 1);
             } else {
+                if constexpr (kShifted) {
+                    at[u] = min(at[u], rows * cols);       // (groups that do not exist)
+                    if (vecs > 0) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[u][e] = load_float(src + (e < n[u] ? at[u] + e : 0));
+                        for (int k = 0; k < 2; ++k) raw[u][k] = __ldg(reinterpret_cast<const uint4*>(src) + min(at[u] / 8 + k, vecs - 1));
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[u][e] = load_float(src + (e < n[u] ? at[u] + e : 0));
+                }
             }
         }
         if constexpr (kRows == kMxAny) {
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < U; ++u) {
+                if constexpr (kShifted) {
+                    mx_shift(raw[u], (int)(at[u] & 7), v[u]);
+                    if (at[u] + 8 > vecs * 8) {            // what is left behind the last whole vector
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[u][e] = e < n[u] ? load_float(src + at[u] + e) : 0.0f;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[u][e] = e < n[u] ? v[u][e] : 0.0f;
+            }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -181,10 +237,16 @@ k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* 
                 *reinterpret_cast<uint32_t*>(codes + (kRows == kMxWhole ? unit * 4 : row[u] * cb + (int64_t)g[u] * 4)) = word;
             } else {
                 uint8_t* to = codes + row[u] * cb + (int64_t)g[u] * 4;
-                for (int e = 0; e < n[u]; e += 2) to[e >> 1] = (uint8_t)(word >> (4 * e));
+                if (cb % 4 == 0) {
+                    *reinterpret_cast<uint32_t*>(to) = word;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        if (e < n[u]) to[e >> 1] = (uint8_t)(word >> (4 * e));
+                }
             }
             if (((kRows == kMxWhole ? (uint32_t)unit : g[u]) & 3) == 0) scales[kRows == kMxWhole ? unit >> 2 : row[u] * nb + (g[u] >> 2)] = (uint8_t)s;
-            if (values) mx_write_values<T, kRows>(values + at[u], word, s, n[u]);
+            if (values) mx_write_values(values + at[u], word, s, n[u], kRows == kMxAny ? mx_store_elements(cols) : 8);
         }
     }
 }
@@ -205,10 +267,11 @@ k_dequantize_mx4(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ 
         if (n == 0) continue;
         uint32_t word = 0;
         if constexpr (kRows != kMxAny) word = __ldcs(reinterpret_cast<const uint32_t*>(codes + (kRows == kMxWhole ? unit * 4 : row * cb + (int64_t)g * 4)));
+        else if (cb % 4 == 0) word = __ldcs(reinterpret_cast<const uint32_t*>(codes + row * cb + (int64_t)g * 4));
         else
             for (int e = 0; e < n; e += 2) word |= (uint32_t)codes[row * cb + (int64_t)g * 4 + (e >> 1)] << (4 * e);
         const int sc = __ldg(scales + (kRows == kMxWhole ? unit >> 2 : row * nb + (g >> 2)));
-        mx_write_values<T, kRows>(values + (kRows == kMxWhole ? unit * 8 : row * cols + (int64_t)g * 8), word, sc, n);
+        mx_write_values(values + (kRows == kMxWhole ? unit * 8 : row * cols + (int64_t)g * 8), word, sc, n, kRows == kMxAny ? mx_store_elements(cols) : 8);
     }
 }
 

@@ -434,3 +434,30 @@ def test_odd_rows_captured_and_in_a_stack():
     stack.close()
     del graph
     layer.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 2), (1, 7), (1, 9), (2, 3), (3, 5), (8, 1), (9, 1), (300, 1), (517, 3), (33, 34), (40, 36), (65, 37), (31, 66),
+                                       (17, 255), (16, 1002), (23, 1001), (200, 44)])
+def test_conversion_of_rows_that_start_anywhere(rows, cols, dtype):
+    """Every place of a row's start in 16 bytes, ends of the array inside a vector, and nothing written behind it."""
+    g = torch.Generator().manual_seed(rows * 131 + cols)
+    w = torch.randn(rows, cols, generator=g).to(dtype).cuda()
+    codes, scales, values = binding.quantize_mx4(w, want_values=True)
+    c_ref, s_ref = mx.quantize(w.float().cpu().numpy())
+    np.testing.assert_array_equal(scales.cpu().numpy(), s_ref)
+    np.testing.assert_array_equal(mx.unpack(codes.cpu().numpy(), cols), c_ref)
+    assert torch.equal(values.cpu(), torch.from_numpy(mx.values(c_ref, s_ref)).to(dtype))
+    cb, nb = (cols + 1) // 2, (cols + 31) // 32
+    c = torch.full((rows * cb + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    s = torch.full((rows * nb + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    v = torch.full((rows * cols + 64,), -7.0, dtype=dtype, device="cuda")
+    L, kind = binding.lib(), 0 if dtype == torch.float32 else 1
+    assert L.fff_quantize_mx4(w.data_ptr(), kind, rows, cols, c.data_ptr(), s.data_ptr(), v.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    for got, want, n, fill in ((c, codes, rows * cb, 0xA5), (s, scales, rows * nb, 0xA5), (v, values, rows * cols, -7.0)):
+        assert torch.equal(got[:n], want.flatten()) and (got[n:] == fill).all()
+    v.fill_(-7.0)
+    assert L.fff_dequantize_mx4(c.data_ptr(), s.data_ptr(), kind, rows, cols, v.data_ptr(), None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(v[:rows * cols], values.flatten()) and (v[rows * cols:] == -7.0).all()
