@@ -155,7 +155,8 @@ fff_status_t fff_create_mx4(fff_handle_t *out, int D, int O, int depth, int leaf
  *   src      [rows, cols]  in, float32 or bfloat16 (dtype)
  *   codes    [rows, (cols + 1) / 2]     out / in: the even column in the low half; the upper half of an odd row's last byte is 0
  *   scales   [rows, (cols + 31) / 32]   out / in: biased exponents
- *   values   [rows, cols]  the numbers that the codes stand for, in dtype; out of fff_quantize_mx4 too, where it may be NULL
+ *   values   [rows, cols]  the numbers that the codes stand for, in dtype; out of fff_quantize_mx4 too, where it may be NULL and must not
+ *                          overlap src (FFF_ERR_INVALID_ARG)
  *
  * The calls use the current device, keep no state and only enqueue one kernel.  rows or cols 0: FFF_OK, nothing is written.
  */

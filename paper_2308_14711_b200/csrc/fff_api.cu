@@ -2388,6 +2388,9 @@ fff_status_t fff_quantize_mx4(const void* src, fff_dtype_t dtype, int64_t rows, 
     fff_status_t s = check_mx4_args(dtype, rows, cols);
     if (s != FFF_OK || rows == 0 || cols == 0) return s;
     if (!src || !codes || !scales || !aligned16(src) || !aligned16(codes) || !aligned16(scales) || !aligned16(values)) return FFF_ERR_INVALID_ARG;
+    // (rows that start anywhere are read by vectors, of which a neighbour may have written its part)
+    const uintptr_t from = reinterpret_cast<uintptr_t>(src), to = reinterpret_cast<uintptr_t>(values), bytes = (uintptr_t)(rows * cols) * (dtype == FFF_DTYPE_F32 ? 4 : 2);
+    if (values && from < to + bytes && to < from + bytes) return FFF_ERR_INVALID_ARG;
     fff::LaunchOn on;
     if ((s = current_device(&on, cuda_stream)) != FFF_OK) return s;
     if (fff::quantize_mx4(on, src, dtype == FFF_DTYPE_F32 ? 4 : 2, rows, cols, codes, scales, values) != cudaSuccess)

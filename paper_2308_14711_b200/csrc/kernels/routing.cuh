@@ -113,32 +113,32 @@ k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_i
                     for (int u = 0; u < U; ++u)
                         if (in >> u & 1) { acc[0] += q[u].x; acc[1] += q[u].y; acc[2] += q[u].z; acc[3] += q[u].w; }
                 }
-                continue;
-            }
-            float m[U][V];
-            TokenFlags flags[U];
+            } else {
+                float m[U][V];
+                TokenFlags flags[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t row = min(b + (int64_t)u * down, b1 - 1);      // (past the end: the last row again)
-                flags[u] = token_flags(leaf_idx, mask, row);
-                if constexpr (V == 4) {
-                    const float4 q = __ldcs(reinterpret_cast<const float4*>(base + row * n_leaves));
-                    m[u][0] = q.x; m[u][1] = q.y; m[u][2] = q.z; m[u][3] = q.w;
-                } else {
-                    m[u][0] = __ldcs(base + row * n_leaves);
+                for (int u = 0; u < U; ++u) {
+                    const int64_t row = min(b + (int64_t)u * down, b1 - 1);      // (past the end: the last row again)
+                    flags[u] = token_flags(leaf_idx, mask, row);
+                    if constexpr (V == 4) {
+                        const float4 q = __ldcs(reinterpret_cast<const float4*>(base + row * n_leaves));
+                        m[u][0] = q.x; m[u][1] = q.y; m[u][2] = q.z; m[u][3] = q.w;
+                    } else {
+                        m[u][0] = __ldcs(base + row * n_leaves);
+                    }
                 }
-            }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const bool in = b + (int64_t)u * down < b1 && flags[u].counts(n_leaves);
+                for (int u = 0; u < U; ++u) {
+                    const bool in = b + (int64_t)u * down < b1 && flags[u].counts(n_leaves);
 #pragma unroll
-                for (int v = 0; v < V; ++v) acc[v] += in ? m[u][v] : 0.0f;
-                mine += in;
-                if constexpr (kHow == kBalFew) {
+                    for (int v = 0; v < V; ++v) acc[v] += in ? m[u][v] : 0.0f;
+                    mine += in;
+                    if constexpr (kHow == kBalFew) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) here[v] += in && flags[u].leaf == c * V + v;
-                } else if (c == 0 && in && (unsigned)(flags[u].leaf - col0) < (unsigned)cols) {
-                    atomicAdd(&s_hist[flags[u].leaf - col0], 1);
+                        for (int v = 0; v < V; ++v) here[v] += in && flags[u].leaf == c * V + v;
+                    } else if (c == 0 && in && (unsigned)(flags[u].leaf - col0) < (unsigned)cols) {
+                        atomicAdd(&s_hist[flags[u].leaf - col0], 1);
+                    }
                 }
             }
         }

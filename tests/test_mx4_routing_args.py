@@ -74,3 +74,9 @@ def test_rows_and_layers_too_long_for_32_bits_are_refused(lib):
     h = C.c_void_p(1234)
     for D, O in ((2 ** 31 - 1, 8), (8, 2 ** 31 - 1), ((1 << 28) + 1, 1)):
         assert lib.fff_create_mx4(C.byref(h), D, O, 0, 1, 0, None, None, FAKE, FAKE, None, FAKE, FAKE, None) == 2 and h.value is None
+
+
+def test_values_do_not_lie_over_their_source(lib):
+    q = lib.fff_quantize_mx4
+    for at in (FAKE, FAKE + 16, FAKE - 16):
+        assert q(FAKE, 1, 3, 5, 0x100000, 0x200000, at, None) == 1
