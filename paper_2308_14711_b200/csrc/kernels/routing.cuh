@@ -11,8 +11,8 @@
 // which needs no logits: one pass over the mixture weights, bottom-up.
 //
 // All three are bound by HBM: 4 B L bytes are read (twice that with a second gradient) or written, a few operations each.  Of 6551 GB/s:
-// loss, 65 536 tokens of 2048 leaves 86.2 us (95 %); its gradient, 16 411 of 2048 24.5 us (84 %); back to the logits, 50 432 tokens of 256
-// leaves 29.3 us (79 %), where issue slots count as well: some 25 instructions per node.
+// loss, 65 536 tokens of 2048 leaves 84.4 us (97 %); its gradient, 16 411 of 2048 24.5 us (84 %); back to the logits, 50 432 tokens of 256
+// leaves 28.4 us (82 %), where issue slots count as well: some 25 instructions per node.
 #pragma once
 
 #include <float.h>

@@ -10,6 +10,8 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -34,6 +36,18 @@ bool matches(const at::Tensor& t, at::ScalarType type, int64_t rows, int64_t col
     if (cols < 0) return t.dim() == 1 && t.size(0) == rows;
     return t.dim() == 2 && t.size(0) == rows && t.size(1) == cols;
 }
+
+// New tensors on the device of one, straight from the allocator where that device is the current one (at::empty finds its way there through the
+// dispatcher: 0.4 us more each, of 6.0 us for fff_balance_loss with three of them).
+struct Fresh {
+    const at::Tensor& like;
+    const bool here;
+    explicit Fresh(const at::Tensor& t) : like(t), here(t.device().index() == c10::cuda::current_device()) {}
+    at::Tensor operator()(at::IntArrayRef sizes, at::ScalarType type) const {
+        if (!here) return at::empty(sizes, like.options().requires_grad(false).dtype(type));
+        return at::Tensor(at::detail::empty_generic(sizes, c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, {}));
+    }
+};
 
 // set_addresses(forward_infer, balance_loss, balance_loss_backward, routing_backward, quantize_mx4)
 PyObject* set_addresses(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -106,8 +120,8 @@ PyObject* balance_loss(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (args[3] == Py_None || !optional(args[3], at::kInt, B, -1, &leaf) || !optional_mask(args[4], B, &mask)) Py_RETURN_NONE;
     void* stream = stream_of(args[5], mix);
     if (PyErr_Occurred()) return nullptr;
-    const auto opt = mix.options().requires_grad(false);
-    at::Tensor loss = at::empty({}, opt), counts = at::empty({L}, opt.dtype(at::kInt)), mean = at::empty({L}, opt);
+    const Fresh fresh(mix);
+    at::Tensor loss = fresh({}, at::kFloat), counts = fresh({L}, at::kInt), mean = fresh({L}, at::kFloat);
     const float* mp = static_cast<const float*>(mix.data_ptr());
     float *lp = static_cast<float*>(loss.data_ptr()), *ep = static_cast<float*>(mean.data_ptr());
     int32_t* cp = static_cast<int32_t*>(counts.data_ptr());
@@ -137,7 +151,7 @@ PyObject* balance_loss_backward(PyObject*, PyObject* const* args, Py_ssize_t n) 
         Py_RETURN_NONE;
     void* stream = stream_of(args[6], leaves);
     if (PyErr_Occurred()) return nullptr;
-    at::Tensor out = at::empty({B, L}, leaves.options().requires_grad(false).dtype(at::kFloat));
+    at::Tensor out = Fresh(leaves)({B, L}, at::kFloat);
     float* op = static_cast<float*>(out.data_ptr());
     int status;
     Py_BEGIN_ALLOW_THREADS
@@ -166,7 +180,7 @@ PyObject* routing_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
         Py_RETURN_NONE;
     void* stream = stream_of(args[8], mix);
     if (PyErr_Occurred()) return nullptr;
-    at::Tensor out = at::empty({B, L - 1}, mix.options().requires_grad(false));
+    at::Tensor out = Fresh(mix)({B, L - 1}, at::kFloat);
     const float* mp = static_cast<const float*>(mix.data_ptr());
     float* op = static_cast<float*>(out.data_ptr());
     int status;
@@ -189,13 +203,13 @@ PyObject* quantize_mx4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     void* stream = stream_of(args[2], w);
     if (want < 0 || PyErr_Occurred()) return nullptr;
     const int64_t cols = w.size(w.dim() - 1), rows = cols > 0 ? w.numel() / cols : 0;
-    const auto opt = w.options().requires_grad(false);
-    std::vector<int64_t> shape(w.sizes().begin(), w.sizes().end());
+    const Fresh fresh(w);
+    at::DimVector shape(w.sizes().begin(), w.sizes().end());
     shape.back() = (cols + 1) / 2;
-    at::Tensor codes = at::empty(shape, opt.dtype(at::kByte));
+    at::Tensor codes = fresh(shape, at::kByte);
     shape.back() = (cols + 31) / 32;
-    at::Tensor scales = at::empty(shape, opt.dtype(at::kByte)), values;
-    if (want) values = at::empty(w.sizes(), opt);
+    at::Tensor scales = fresh(shape, at::kByte), values;
+    if (want) values = fresh(w.sizes(), w.scalar_type());
     const void* wp = w.data_ptr();
     uint8_t *cp = static_cast<uint8_t*>(codes.data_ptr()), *sp = static_cast<uint8_t*>(scales.data_ptr());
     void* vp = want ? values.data_ptr() : nullptr;
@@ -231,9 +245,9 @@ PyObject* forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     else stream = PyLong_AsVoidPtr(args[8]);
     if (PyErr_Occurred()) return nullptr;
     if (args[5] != Py_None) y = THPVariable_Unpack(args[5]);
-    else y = at::empty({B, O}, x.options().requires_grad(false));
+    else y = Fresh(x)({B, O}, type);
     if (args[6] != Py_None) leaf = THPVariable_Unpack(args[6]);
-    else if (want_leaf) leaf = at::empty({B}, x.options().requires_grad(false).dtype(at::kInt));
+    else if (want_leaf) leaf = Fresh(x)({B}, at::kInt);
     const void* xp = x.data_ptr();
     void* yp = y.data_ptr();
     int32_t* lp = leaf.defined() ? static_cast<int32_t*>(leaf.data_ptr()) : nullptr;
