@@ -409,3 +409,43 @@ def test_calls_that_are_refused(call):
     assert lib.fff_routing_backward(h, p(mix), p(mix), None, None, None, None, p(out) + 8, 10, None) == 1
     assert lib.fff_balance_loss(h, p(mix), p(leaf), None, None, None, None, 10, None) == 0          # nothing asked for
     layer.close()
+
+
+# sizes at which the kernels change their ways: a row per warp from 128 leaves on, rows by warps up to 512 and by CTAs (several at a time, the last
+# group not full) above, slopes in shared memory up to 8192, more than 256 rows in a sum, several groups of slices
+MORE_SIZES = [(0, 600), (2, 70001), (5, 3000), (6, 9001), (7, 127), (7, 40001), (8, 3), (9, 5000), (10, 64), (10, 1003), (11, 597), (12, 333),
+              (13, 333), (14, 21), (16, 2)]
+
+
+@pytest.mark.parametrize("kind", ["mask", "out_of_range"])
+@pytest.mark.parametrize("depth,B", MORE_SIZES)
+def test_balance_loss_where_its_ways_change(depth, B, kind):
+    test_balance_loss(depth, B, kind)
+
+
+@pytest.mark.parametrize("kind", ["upstream", "balance", "both_masked"])
+@pytest.mark.parametrize("depth,B", MORE_SIZES)
+def test_routing_backward_where_its_ways_change(depth, B, kind):
+    test_routing_backward(depth, B, kind)
+
+
+def test_rows_and_gradients_end_where_they_end():
+    """Nothing behind the last row is written, and what lies behind the last row of the mixture weights is not used."""
+    for depth, B in ((1, 77), (3, 61), (8, 5), (9, 3), (10, 1001), (11, 3), (13, 2)):
+        L = 1 << depth
+        mix, leaf, layer = mixture(B, depth, 7, 1.0), leaves(B, depth, 7), tree(depth)
+        wide = torch.full((B * L + 4096,), float("nan"), device="cuda")
+        wide[:B * L] = gpu(mix).flatten()
+        x = wide[:B * L].view(B, L)
+        loss, counts, mean = layer.balance_loss(x, gpu(leaf))
+        want = layer.balance_loss(gpu(mix), gpu(leaf))
+        assert float(loss) == float(want[0]) and torch.equal(mean, want[2])
+        out, d = torch.full((B * (L - 1) + 64,), 7.0, device="cuda"), torch.full((B * L + 64,), 7.0, device="cuda")
+        dloss, stream = torch.tensor([0.5], device="cuda"), torch.cuda.current_stream().cuda_stream
+        lib, h, idx = binding.lib(), layer._h, gpu(leaf)
+        assert lib.fff_routing_backward(h, x.data_ptr(), None, idx.data_ptr(), None, counts.data_ptr(), dloss.data_ptr(), out.data_ptr(), B, stream) == 0
+        assert lib.fff_balance_loss_backward(h, idx.data_ptr(), None, counts.data_ptr(), dloss.data_ptr(), d.data_ptr(), B, stream) == 0
+        torch.cuda.synchronize()
+        assert (out[B * (L - 1):] == 7.0).all() and (d[B * L:] == 7.0).all()
+        assert torch.equal(out[:B * (L - 1)].view(B, L - 1), layer.routing_backward(gpu(mix), leaf_idx=idx, counts=counts, dloss=dloss))
+        layer.close()
