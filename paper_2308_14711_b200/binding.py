@@ -241,6 +241,22 @@ def _stream_of(t, stream):
     return stream.cuda_stream if stream is not None else _torch()._C._cuda_getCurrentRawStream(t.device.index)
 
 
+def _fresh(stream, shape, dtype, device):
+    """A tensor for a result, memory of the stream that writes it: memory of another one may still be read there for whoever had it before.
+    The current stream, which may read it, is noted, so that it may be dropped at any time."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.Stream):               # (something else with an address)
+        at = stream.cuda_stream
+        stream = torch.cuda.ExternalStream(at, device=device) if at else torch.cuda.default_stream(device)
+    current = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(current)
+    return t
+
+
 def _on_device(t):
     """Makes the tensor's device the current one (nothing to do where it is)."""
     torch = _torch()
@@ -274,9 +290,9 @@ def quantize_mx4(w, want_values: bool = False, stream=None):
         raise ValueError("w: expected rows")
     cols, lead = w.shape[-1], tuple(w.shape[:-1])
     dtype, wp = _mx4_dtype(w.dtype), _ptr(w, w.dtype, w.shape, "w")
-    codes = torch.empty(lead + ((cols + 1) // 2,), dtype=torch.uint8, device=w.device)
-    scales = torch.empty(lead + ((cols + 31) // 32,), dtype=torch.uint8, device=w.device)
-    values = torch.empty_like(w, memory_format=torch.contiguous_format) if want_values else None
+    codes = _fresh(stream, lead + ((cols + 1) // 2,), torch.uint8, w.device)
+    scales = _fresh(stream, lead + ((cols + 31) // 32,), torch.uint8, w.device)
+    values = _fresh(stream, w.shape, w.dtype, w.device) if want_values else None
     with _on_device(w):
         _check(lib().fff_quantize_mx4(wp, dtype, w.numel() // max(cols, 1), cols, codes.data_ptr(), scales.data_ptr(),
                                       None if values is None else values.data_ptr(), _stream_of(w, stream)), "fff_quantize_mx4")
@@ -291,7 +307,7 @@ def dequantize_mx4(codes, scales, cols: int, dtype=None, stream=None):
     d = _mx4_dtype(dtype)
     cp = _ptr(codes, torch.uint8, lead + ((cols + 1) // 2,), "codes")
     sp = _ptr(scales, torch.uint8, lead + ((cols + 31) // 32,), "scales")
-    values = torch.empty(lead + (cols,), dtype=dtype, device=codes.device)
+    values = _fresh(stream, lead + (cols,), dtype, codes.device)
     with _on_device(codes):
         _check(lib().fff_dequantize_mx4(cp, sp, d, values.numel() // max(cols, 1), cols, values.data_ptr(), _stream_of(codes, stream)),
                "fff_dequantize_mx4")
@@ -299,7 +315,10 @@ def dequantize_mx4(codes, scales, cols: int, dtype=None, stream=None):
 
 
 class FFFLayer:
-    """One FFF layer on the current CUDA device; tensors in, tensors out, all work in libfff.so."""
+    """One FFF layer on the current CUDA device; tensors in, tensors out, all work in libfff.so.
+
+    Calls take stream= (a torch.cuda.Stream; the current one without).  It has to come after what makes their arguments, which have to live
+    until it is done with them; results that a call allocates may be dropped at any time."""
 
     def __init__(self, D: int, O: int, depth: int, leaf_width: int, activation: str, dtype: str,
                  node_w, node_b, w1, b1, w2, b2, path: str = "auto", w1_scale=None, w2_scale=None):
@@ -406,9 +425,9 @@ class FFFLayer:
         B = x.shape[0]
         xp = _ptr(x, self.tdtype, (B, self.D), "x")
         if y is None:
-            y = torch.empty((B, self.O), dtype=self.tdtype, device=x.device)
+            y = _fresh(stream, (B, self.O), self.tdtype, x.device)
         if leaf_idx is None and want_leaf_idx:
-            leaf_idx = torch.empty((B,), dtype=torch.int32, device=x.device)
+            leaf_idx = _fresh(stream, (B,), torch.int32, x.device)
         fff_forward_infer(self._h, xp, _ptr(y, self.tdtype, (B, self.O), "y"), _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"), B,
                           self._stream(stream))
         return y, leaf_idx
@@ -417,9 +436,9 @@ class FFFLayer:
         """FORWARD_T: returns (y, mixture weights float32 [B, 2^d] or None, node entropies float32 [2^d - 1] or None)."""
         torch = _torch()
         B = x.shape[0]
-        y = torch.empty((B, self.O), dtype=self.tdtype, device=x.device)
-        mix = torch.empty((B, self.n_leaves), dtype=torch.float32, device=x.device) if want_mixture else None
-        ent = torch.empty((max(self.n_leaves - 1, 1),), dtype=torch.float32, device=x.device) if want_entropy else None
+        y = _fresh(stream, (B, self.O), self.tdtype, x.device)
+        mix = _fresh(stream, (B, self.n_leaves), torch.float32, x.device) if want_mixture else None
+        ent = _fresh(stream, (max(self.n_leaves - 1, 1),), torch.float32, x.device) if want_entropy else None
         _check(lib().fff_forward_train(self._h, _ptr(x, self.tdtype, (B, self.D), "x"), y.data_ptr(),
                                        None if mix is None else mix.data_ptr(), None if ent is None else ent.data_ptr(), B,
                                        self._stream(stream)), "fff_forward_train")
@@ -436,9 +455,9 @@ class FFFLayer:
         torch = _torch()
         B, dev = mixture.shape[0], mixture.device
         mp, lp = _ptr(mixture, torch.float32, (B, self.n_leaves), "mixture"), _ptr(leaf_idx, torch.int32, (B,), "leaf_idx")
-        loss = torch.empty((), dtype=torch.float32, device=dev)
-        counts = torch.empty((self.n_leaves,), dtype=torch.int32, device=dev)
-        mean = torch.empty((self.n_leaves,), dtype=torch.float32, device=dev)
+        loss = _fresh(stream, (), torch.float32, dev)
+        counts = _fresh(stream, (self.n_leaves,), torch.int32, dev)
+        mean = _fresh(stream, (self.n_leaves,), torch.float32, dev)
         _check(lib().fff_balance_loss(self._h, mp, lp, _mask_ptr(token_mask, B), loss.data_ptr(), counts.data_ptr(), mean.data_ptr(), B,
                                       _stream_of(mixture, stream)), "fff_balance_loss")
         return loss, counts, mean
@@ -455,7 +474,7 @@ class FFFLayer:
         B = leaf_idx.shape[0]
         lp, cp = _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"), _ptr(counts, torch.int32, (self.n_leaves,), "counts")
         gp = _ptr(dloss, torch.float32, dloss.shape if dloss.numel() == 1 else (1,), "dloss")
-        out = torch.empty((B, self.n_leaves), dtype=torch.float32, device=leaf_idx.device)
+        out = _fresh(stream, (B, self.n_leaves), torch.float32, leaf_idx.device)
         _check(lib().fff_balance_loss_backward(self._h, lp, _mask_ptr(token_mask, B), cp, gp, out.data_ptr(), B, _stream_of(leaf_idx, stream)),
                "fff_balance_loss_backward")
         return out
@@ -475,7 +494,7 @@ class FFFLayer:
         mp, dp = _ptr(mixture, f32, (B, self.n_leaves), "mixture"), _ptr(dmixture, f32, (B, self.n_leaves), "dmixture")
         lp, cp = _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"), _ptr(counts, torch.int32, (self.n_leaves,), "counts")
         gp = None if dloss is None else _ptr(dloss, f32, dloss.shape if dloss.numel() == 1 else (1,), "dloss")
-        out = torch.empty((B, self.n_leaves - 1), dtype=f32, device=mixture.device)
+        out = _fresh(stream, (B, self.n_leaves - 1), f32, mixture.device)
         _check(lib().fff_routing_backward(self._h, mp, dp, lp, _mask_ptr(token_mask, B), cp, gp, out.data_ptr(), B, _stream_of(mixture, stream)),
                "fff_routing_backward")
         return out
@@ -493,7 +512,7 @@ class FFFLayer:
         torch = _torch()
         B = x.shape[0]
         if leaf_idx is None:
-            leaf_idx = torch.empty((B,), dtype=torch.int32, device=x.device)
+            leaf_idx = _fresh(stream, (B,), torch.int32, x.device)
         fff_tree_descent(self._h, _ptr(x, self.tdtype, (B, self.D), "x"), _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"),
                          B, self._stream(stream))
         return leaf_idx
@@ -501,8 +520,8 @@ class FFFLayer:
     def leaf_bucketing(self, leaf_idx, stream=None):
         torch = _torch()
         B = leaf_idx.shape[0]
-        offsets = torch.empty((self.n_leaves + 1,), dtype=torch.int32, device=leaf_idx.device)
-        perm = torch.empty((B,), dtype=torch.int32, device=leaf_idx.device)
+        offsets = _fresh(stream, (self.n_leaves + 1,), torch.int32, leaf_idx.device)
+        perm = _fresh(stream, (B,), torch.int32, leaf_idx.device)
         fff_leaf_bucketing(self._h, _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"), offsets.data_ptr(), perm.data_ptr(),
                            B, self._stream(stream))
         return offsets, perm
@@ -511,7 +530,7 @@ class FFFLayer:
         torch = _torch()
         B = x.shape[0]
         if y is None:
-            y = torch.empty((B, self.O), dtype=self.tdtype, device=x.device)
+            y = _fresh(stream, (B, self.O), self.tdtype, x.device)
         fff_grouped_leaf_ff(self._h, _ptr(x, self.tdtype, (B, self.D), "x"),
                             _ptr(leaf_idx, torch.int32, (B,), "leaf_idx"),
                             _ptr(offsets, torch.int32, (self.n_leaves + 1,), "offsets"),
@@ -521,8 +540,8 @@ class FFFLayer:
 
     def last_bucketing(self, B: int, stream=None):
         torch = _torch()
-        perm = torch.empty((B,), dtype=torch.int32, device="cuda")
-        offsets = torch.empty((self.n_leaves + 1,), dtype=torch.int32, device="cuda")
+        perm = _fresh(stream, (B,), torch.int32, torch.device("cuda", torch.cuda.current_device()))
+        offsets = _fresh(stream, (self.n_leaves + 1,), torch.int32, perm.device)
         fff_debug_get_bucketing(self._h, perm.data_ptr(), offsets.data_ptr(), self._stream(stream))
         return offsets, perm
 
@@ -580,9 +599,9 @@ class FFFStack:
         torch = _torch()
         B = x.shape[0]
         if y is None:
-            y = torch.empty((B, self.D), dtype=self.tdtype, device=x.device)
+            y = _fresh(stream, (B, self.D), self.tdtype, x.device)
         if leaf_idx is None and want_leaf_idx:
-            leaf_idx = torch.empty((len(self.layers), B), dtype=torch.int32, device=x.device)
+            leaf_idx = _fresh(stream, (len(self.layers), B), torch.int32, x.device)
         st = _stream_ptr(stream)
         _check(lib().fff_stack_forward(self._s, _ptr(x, self.tdtype, (B, self.D), "x"), _ptr(y, self.tdtype, (B, self.D), "y"),
                                        _ptr(leaf_idx, torch.int32, (len(self.layers), B), "leaf_idx"), B, st), "fff_stack_forward")

@@ -13,6 +13,7 @@
 #include <ATen/EmptyTensor.h>
 #include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -39,11 +40,27 @@ bool matches(const at::Tensor& t, at::ScalarType type, int64_t rows, int64_t col
 
 // New tensors on the device of one, straight from the allocator where that device is the current one (at::empty finds its way there through the
 // dispatcher: 0.4 us more each, of 6.0 us for fff_balance_loss with three of them).
+// They are memory of the stream that writes them (its address is an argument, or None for the current one): memory of another stream may still be
+// read there for whoever had it before.  The current stream, which may read them, is noted, so that they may be dropped at any time.
 struct Fresh {
     const at::Tensor& like;
-    const bool here;
-    explicit Fresh(const at::Tensor& t) : like(t), here(t.device().index() == c10::cuda::current_device()) {}
+    const bool here, elsewhere;
+    void* const stream;
+    Fresh(const at::Tensor& t, PyObject* arg, void* st) : like(t), here(t.device().index() == c10::cuda::current_device()), elsewhere(arg != Py_None), stream(st) {}
     at::Tensor operator()(at::IntArrayRef sizes, at::ScalarType type) const {
+        if (!elsewhere) return make(sizes, type);
+        const auto device = like.device().index();
+        const c10::cuda::CUDAStream current = c10::cuda::getCurrentCUDAStream(device);
+        at::Tensor t;
+        {
+            c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), device));
+            t = at::empty(sizes, like.options().requires_grad(false).dtype(type));
+        }
+        c10::cuda::CUDACachingAllocator::recordStream(t.storage().data_ptr(), current);
+        return t;
+    }
+private:
+    at::Tensor make(at::IntArrayRef sizes, at::ScalarType type) const {
         if (!here) return at::empty(sizes, like.options().requires_grad(false).dtype(type));
         return at::Tensor(at::detail::empty_generic(sizes, c10::cuda::CUDACachingAllocator::get(), c10::DispatchKeySet(c10::DispatchKey::CUDA), type, {}));
     }
@@ -120,7 +137,7 @@ PyObject* balance_loss(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (args[3] == Py_None || !optional(args[3], at::kInt, B, -1, &leaf) || !optional_mask(args[4], B, &mask)) Py_RETURN_NONE;
     void* stream = stream_of(args[5], mix);
     if (PyErr_Occurred()) return nullptr;
-    const Fresh fresh(mix);
+    const Fresh fresh(mix, args[5], stream);
     at::Tensor loss = fresh({}, at::kFloat), counts = fresh({L}, at::kInt), mean = fresh({L}, at::kFloat);
     const float* mp = static_cast<const float*>(mix.data_ptr());
     float *lp = static_cast<float*>(loss.data_ptr()), *ep = static_cast<float*>(mean.data_ptr());
@@ -151,7 +168,7 @@ PyObject* balance_loss_backward(PyObject*, PyObject* const* args, Py_ssize_t n) 
         Py_RETURN_NONE;
     void* stream = stream_of(args[6], leaves);
     if (PyErr_Occurred()) return nullptr;
-    at::Tensor out = Fresh(leaves)({B, L}, at::kFloat);
+    at::Tensor out = Fresh(leaves, args[6], stream)({B, L}, at::kFloat);
     float* op = static_cast<float*>(out.data_ptr());
     int status;
     Py_BEGIN_ALLOW_THREADS
@@ -180,7 +197,7 @@ PyObject* routing_backward(PyObject*, PyObject* const* args, Py_ssize_t n) {
         Py_RETURN_NONE;
     void* stream = stream_of(args[8], mix);
     if (PyErr_Occurred()) return nullptr;
-    at::Tensor out = Fresh(mix)({B, L - 1}, at::kFloat);
+    at::Tensor out = Fresh(mix, args[8], stream)({B, L - 1}, at::kFloat);
     const float* mp = static_cast<const float*>(mix.data_ptr());
     float* op = static_cast<float*>(out.data_ptr());
     int status;
@@ -203,7 +220,7 @@ PyObject* quantize_mx4(PyObject*, PyObject* const* args, Py_ssize_t n) {
     void* stream = stream_of(args[2], w);
     if (want < 0 || PyErr_Occurred()) return nullptr;
     const int64_t cols = w.size(w.dim() - 1), rows = cols > 0 ? w.numel() / cols : 0;
-    const Fresh fresh(w);
+    const Fresh fresh(w, args[2], stream);
     at::DimVector shape(w.sizes().begin(), w.sizes().end());
     shape.back() = (cols + 1) / 2;
     at::Tensor codes = fresh(shape, at::kByte);
@@ -245,9 +262,9 @@ PyObject* forward(PyObject*, PyObject* const* args, Py_ssize_t n) {
     else stream = PyLong_AsVoidPtr(args[8]);
     if (PyErr_Occurred()) return nullptr;
     if (args[5] != Py_None) y = THPVariable_Unpack(args[5]);
-    else y = Fresh(x)({B, O}, type);
+    else y = Fresh(x, args[8], stream)({B, O}, type);
     if (args[6] != Py_None) leaf = THPVariable_Unpack(args[6]);
-    else if (want_leaf) leaf = Fresh(x)({B}, at::kInt);
+    else if (want_leaf) leaf = Fresh(x, args[8], stream)({B}, at::kInt);
     const void* xp = x.data_ptr();
     void* yp = y.data_ptr();
     int32_t* lp = leaf.defined() ? static_cast<int32_t*>(leaf.data_ptr()) : nullptr;
