@@ -101,7 +101,8 @@ typedef enum {
  * kernels reads: bf16 layers with tensor-core kernels have images of all
  * weights beside the plain ones, float32 layers with a one-launch kernel on
  * bulk copies (most of 128 columns and more) leaf_w2 once more, transposed.
- * The call synchronises the device.  On failure *out is NULL.
+ * The call synchronises the device, before it reads the arrays (work on any
+ * stream that writes them may still be enqueued) and at its end.  On failure *out is NULL.
  */
 fff_status_t fff_create(fff_handle_t *out, int D, int O, int depth, int leaf_width,
                         fff_activation_t act, fff_dtype_t dtype,
@@ -470,7 +471,7 @@ const char *fff_profile_launch_name(fff_handle_t h, int i);
  *
  *   layers     n_layers distinct live handles on one device, one element type, D == O == the same width
  *   ln_gamma   NULL, or n_layers device pointers to [D] vectors in the element type (an entry may be NULL = ones)
- *   ln_beta    likewise (NULL = zeros); both are copied.  Ignored when layer_norm == 0
+ *   ln_beta    likewise (NULL = zeros); both are copied, once the device has done what may write them.  Ignored when layer_norm == 0
  * The stack does not own the layers: destroy it before them, and run no other forward on them while one of
  * the stack's is in flight.  fff_set_path / fff_set_tuning on the layers stay in effect.
  */

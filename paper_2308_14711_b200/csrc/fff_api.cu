@@ -1954,6 +1954,8 @@ fff_status_t create_common(fff_handle_t* out, int D, int O, int depth, int leaf_
     if (!h) return FFF_ERR_ALLOC;
     if (cudaGetDevice(&h->device) != cudaSuccess) { delete h; return cudaGetLastError(), FFF_ERR_CUDA; }
     if (h->device < 0 || h->device >= kMaxDevices) { delete h; return FFF_ERR_UNSUPPORTED; }
+    // the arrays may be results of work that a non-blocking stream has still to do: the copies below, on the default stream, would not wait for it
+    if (cudaDeviceSynchronize() != cudaSuccess) { delete h; return cudaGetLastError(), FFF_ERR_CUDA; }
     cudaDeviceGetAttribute(&h->sm_count, cudaDevAttrMultiProcessorCount, h->device);
     {
         const int smem_max = (int)(sizeof(int) * (fff::kBucketWarps + 1) * fff::kBucketMaxBinsPerCta);
@@ -2737,6 +2739,7 @@ fff_status_t fff_stack_create(fff_stack_t* out, int n_layers, const fff_handle_t
     s->beta.assign(n_layers, nullptr);
     DeviceGuard g(s->device);
     fff_status_t rc = FFF_OK;
+    if (cudaDeviceSynchronize() != cudaSuccess) rc = (cudaGetLastError(), FFF_ERR_CUDA);      // (the vectors may still be on their way, as in create_common)
     for (int k = 0; k < n_layers && rc == FFF_OK && s->layer_norm; ++k) {
         if (ln_gamma && ln_gamma[k]) rc = clone(&s->gamma[k], ln_gamma[k], (size_t)s->D * s->esize);
         if (rc == FFF_OK && ln_beta && ln_beta[k]) rc = clone(&s->beta[k], ln_beta[k], (size_t)s->D * s->esize);
