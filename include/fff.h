@@ -136,7 +136,7 @@ fff_status_t fff_create_w8(fff_handle_t *out, int D, int O, int depth, int leaf_
  *                                                            mostly scales)
  *
  * A weight is the value of its code times 2^(scale - 127), exactly; a block with scale 255 is NaN, a product too large for bfloat16
- * infinite.  Everything else (x, y, node weights, biases) is bfloat16; products are accumulated in float32, hidden values keep
+ * infinite (hidden values below 2^-134 count as 0 behind such weights of W2).  Everything else (x, y, node weights, biases) is bfloat16; products are accumulated in float32, hidden values keep
  * float32 precision to 2^-16.  (The paper stores its weights in one floating-point type; this takes 17/64 of bfloat16's bytes.)
  * Any D, O and depth; FFF_ERR_UNSUPPORTED for l > 1024 and for leaves of 2^28 bytes and more.  Rows of x and y that are no 16-byte
  * vectors (D % 8, O % 8) go through a workspace of B rounded-up rows, but for small batches.  fff_forward_train is not available on such a

@@ -66,6 +66,8 @@ __device__ __forceinline__ uint32_t mx_mul1(uint32_t byte, bool big) { return (b
 __device__ __forceinline__ uint32_t mx_mul2(uint32_t byte) {
     return byte == 255 ? 0x7fff7fffu : (byte > 128u ? byte - 1u : 127u) * 0x00800080u;
 }
+// Two bf16 values, infinities and NaN as zeros.
+__device__ __forceinline__ uint32_t mx_finite(uint32_t two) { return two & ~__vcmpeq2(two & 0x7f807f80u, 0x7f807f80u); }
 // The values of a word's first n codes, times the scale of byte s.  `each`: elements that a store may have, as n and the place are
 // multiples of them: 8 or 4; or 1, and then neighbours go in pairs where they lie on an even place.
 template <typename T>
@@ -574,7 +576,13 @@ __device__ __forceinline__ void mx_outputs(__nv_bfloat16* __restrict__ y, bool y
             }
         }
         uint32_t w[8][P];                              // [2 i + row][pair of hidden units]
+        bool infinite = false;                         // (kBig) some of them may be: scales of 2^126 and more
         auto operands = [&]() {
+            if constexpr (kBig) {
+                unsigned huge = __vcmpgeu4(next.sc.x, 0xfdfdfdfdu);
+                if constexpr (!K16) huge |= __vcmpgeu4(next.sc.y, 0xfdfdfdfdu);
+                infinite = __any_sync(kFullMask, huge);
+            }
             uint32_t f1[P], f2[P];                     // the scales of a pair of hidden units are neighbouring bytes
 #pragma unroll
             for (int p = 0; p < P; ++p) {
@@ -622,6 +630,16 @@ __device__ __forceinline__ void mx_outputs(__nv_bfloat16* __restrict__ y, bool y
                         else ptx::mma_bf16(acc[t][i], w[2 * i][pair], w[2 * i + 1][pair], w[2 * i][pair + 1], w[2 * i + 1][pair + 1], b[t][0], b[t][1]);
                     }
             };
+            // The same without weights that are no numbers, for the second summand of the hidden values: an infinite weight times the first
+            // is the product, and one of the second, of the other sign or zero, would make a NaN of it.
+            auto multiply_finite = [&](int pair, const uint32_t (&b)[TG][2]) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t f[4] = {mx_finite(w[2 * i][pair]), mx_finite(w[2 * i + 1][pair]), mx_finite(w[2 * i][pair + 1]), mx_finite(w[2 * i + 1][pair + 1])};
+#pragma unroll
+                    for (int t = 0; t < TG; ++t) ptx::mma_bf16(acc[t][i], f[0], f[1], f[2], f[3], b[t][0], b[t][1]);
+                }
+            };
             for (int kb = 0; kb < kblocks; ++kb) {
                 if (kWide) {
                     operands();
@@ -641,6 +659,11 @@ __device__ __forceinline__ void mx_outputs(__nv_bfloat16* __restrict__ y, bool y
                             const uint4 q = *reinterpret_cast<const uint4*>(from);
                             b[0][t][0] = q.x; b[0][t][1] = q.y; b[1][t][0] = q.z; b[1][t][1] = q.w;
                         }
+                    }
+                    if (kBig && p == 1 && infinite) {
+                        multiply_finite(0, b[0]);
+                        if constexpr (!K16) multiply_finite(2, b[1]);
+                        continue;
                     }
                     multiply(0, b[0], !kWide && p == 0);
                     if constexpr (!K16) multiply(2, b[1], false);

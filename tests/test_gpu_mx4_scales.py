@@ -1,4 +1,4 @@
-"""4-bit layers whose scales are far from 1: over 2, or NaN; in every kernel that reads them (a
+"""4-bit layers whose scales are far from 1: over 2, NaN, or so large that weights are infinite in bfloat16; in every kernel that reads them (a
 CTA per token for small batches, tiles of a leaf's tokens, a warp per token for thin leaves), and through the stage call.  Outputs are compared
 element by element under the bounds of tests/test_gpu_mx4.py, which are relative to sums of magnitudes and so hold for scales of any size."""
 import numpy as np
@@ -64,4 +64,32 @@ def test_a_nan_block_of_w1_makes_its_leaf_nan(l, activation, B):
     y_ref, bound = expected(cfg, w, one[2], two[2], x_host, leaf)
     for got in (y, staged):
         assert np.isnan(got[~ok]).all() and (np.abs(got[ok] - y_ref[ok]) <= bound[ok]).all()
+    layer.close()
+
+
+@pytest.mark.parametrize("B", [FEW, MANY])
+@pytest.mark.parametrize("activation", ["gelu", "relu"])
+@pytest.mark.parametrize("l", [3, 8, 12, 32, 70])
+def test_infinite_output_weights(l, activation, B):
+    """Scale 254 makes codes of 2 and more infinite: h times infinity of h's sign, NaN where h is 0, whatever the leaf's width; blocks beside it
+    keep their values."""
+    cfg = C("inf", 128, 96, 2, l, activation, "bf16", B, "normal")
+    w, one, two, net, x_host = make(cfg, seed=8)
+    bad, unit = 1, l // 2
+    codes, scales = two[0].copy(), two[1].copy()
+    scales[bad, unit, 1] = 254                             # outputs 32 to 63
+    codes[bad, unit, 32:64] = np.arange(32) % 8 // 4 * 4 + np.arange(32) % 4 * (np.arange(32) % 8 // 4) | np.arange(32) // 16 * 8      # 0 or 2, 3, 4, 6, both signs
+    assert set(codes[bad, unit, 32:64] & 7) == {0, 4, 5, 6, 7}
+    v2 = mx.values(codes, scales)
+    v2 = np.where(np.abs(v2) >= 2.0 ** 128, np.copysign(np.inf, v2), v2)
+    layer = layer_of(cfg, w, one, (codes, scales))
+    y, staged, leaf = run(layer, util.to_device(x_host, "bf16"))
+    assert (leaf == bad).any()
+    with np.errstate(invalid="ignore"):
+        y_ref, bound = expected(cfg, w, one[2], v2, x_host, leaf)
+    finite = np.isfinite(y_ref)
+    assert np.isinf(y_ref).any() and (np.isnan(y_ref).any() == (activation == "relu"))
+    for got in (y, staged):
+        assert (np.abs(got[finite] - y_ref[finite]) <= bound[finite]).all()
+        np.testing.assert_array_equal(got[~finite], y_ref[~finite])          # (NaN where NaN, infinities of the same sign)
     layer.close()
