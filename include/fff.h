@@ -424,7 +424,8 @@ fff_status_t fff_selftest_bounded_wait(fff_handle_t h, int64_t limit_cycles, voi
 typedef enum {
     FFF_CAP_TENSOR_DESCENT = 1,   /* staged descent on tensor cores (bf16, D % 128 == 0, depth > 0) */
     FFF_CAP_TCGEN05_DESCENT = 2,  /* ... its first stage on tcgen05 */
-    FFF_CAP_TENSOR_LEAF = 4,      /* grouped leaf evaluation on tensor cores (also O % 8 == 0, l <= 64; 4-bit leaf weights: l >= 8) */
+    FFF_CAP_TENSOR_LEAF = 4,      /* grouped leaf evaluation on tensor cores (also O % 8 == 0, l <= 64; 4-bit leaf weights: also O % 8 == 0,
+                                     l >= 8, and with other O they run there too, on rows of y that are copied) */
     FFF_CAP_TCGEN05_LEAF = 8,     /* ... on tcgen05 (also O % 16 == 0) */
     FFF_CAP_FUSED_SMALL = 16,     /* FFF_PATH_FUSED may be set: small trees with thin leaves and rows that are not too wide (l <= 32;
                                      2^depth leaves of l, rounded up to a power of two, hold at most 32 neurons per SM;

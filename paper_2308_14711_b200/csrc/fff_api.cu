@@ -2575,10 +2575,11 @@ int fff_last_launch_count(fff_handle_t h) { return live(h) ? h->launches : -1; }
 int fff_capabilities(fff_handle_t h) {
     if (!live(h)) return -1;
     int caps = 0;
-    if (h->D == h->Dp) {
+    // (x_cols: 4-bit layers round D up, and copy rows of x and y that are no whole vectors)
+    if (h->x_cols == h->Dp) {
         if (!h->stages.empty() || !h->ustages.empty()) caps |= FFF_CAP_TENSOR_DESCENT;
         if (!h->ustages.empty()) caps |= FFF_CAP_TCGEN05_DESCENT;
-        if (h->LP != 0 || h->mx.mma) caps |= FFF_CAP_TENSOR_LEAF;
+        if (h->LP != 0 || (h->mx.mma && h->O % 8 == 0)) caps |= FFF_CAP_TENSOR_LEAF;
         if (h->w2uimg || h->w2codes) caps |= FFF_CAP_TCGEN05_LEAF;
     } else if (!h->ustages.empty() || h->LP != 0 || h->mx.mma) {
         caps |= FFF_CAP_PADDED;
