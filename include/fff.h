@@ -156,8 +156,9 @@ fff_status_t fff_create_mx4(fff_handle_t *out, int D, int O, int depth, int leaf
  *   src      [rows, cols]  in, float32 or bfloat16 (dtype)
  *   codes    [rows, (cols + 1) / 2]     out / in: the even column in the low half; the upper half of an odd row's last byte is 0
  *   scales   [rows, (cols + 31) / 32]   out / in: biased exponents
- *   values   [rows, cols]  the numbers that the codes stand for, in dtype; out of fff_quantize_mx4 too, where it may be NULL and must not
- *                          overlap src (FFF_ERR_INVALID_ARG)
+ *   values   [rows, cols]  the numbers that the codes stand for, in dtype; out of fff_quantize_mx4 too, where it may be NULL
+ *
+ * Outputs overlap no input (FFF_ERR_INVALID_ARG).
  *
  * The calls use the current device, keep no state and only enqueue one kernel.  rows or cols 0: FFF_OK, nothing is written.
  */
@@ -253,7 +254,8 @@ fff_status_t fff_balance_loss_backward(fff_handle_t h, const int32_t *leaf_idx, 
  *   dmixture     [B, 2^d]       in, may be NULL where counts and dloss are given
  *   counts, dloss               in, both or neither: adds the gradient of the balance loss without its matrix; leaf_idx (may be NULL) as above
  *   token_mask   [B]            in, may be NULL: the rows of masked tokens become 0, whatever they hold
- *   dlogits      [B, 2^d - 1]   out, rows dense, nodes in the order of node_w.  Nothing is written for depth 0
+ *   dlogits      [B, 2^d - 1]   out, rows dense, nodes in the order of node_w; overlaps neither mixture nor dmixture (FFF_ERR_INVALID_ARG).
+ *                               Nothing is written for depth 0
  */
 fff_status_t fff_routing_backward(fff_handle_t h, const float *mixture, const float *dmixture, const int32_t *leaf_idx,
                                   const uint8_t *token_mask, const int32_t *counts, const float *dloss, float *dlogits, int64_t B,

@@ -2307,6 +2307,11 @@ fff_status_t fff_forward_train(fff_handle_t h, const void* x, void* y, float* mi
 // ---- routing losses
 
 static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+// Whether na bytes from a on and nb bytes from b on have one in common (either may be NULL).
+static bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return a && b && p < q + (uintptr_t)nb && q < p + (uintptr_t)na;
+}
 
 fff_status_t fff_balance_loss(fff_handle_t h, const float* mixture, const int32_t* leaf_idx, const uint8_t* token_mask, float* loss,
                               int32_t* counts, float* mean_mixture, int64_t B, void* cuda_stream) {
@@ -2351,6 +2356,9 @@ fff_status_t fff_routing_backward(fff_handle_t h, const float* mixture, const fl
     if (!mixture || !dlogits || !aligned16(mixture) || !aligned16(dmixture) || !aligned16(dlogits) || !aligned4(counts) || !aligned4(dloss) ||
         !aligned4(leaf_idx))
         return FFF_ERR_INVALID_ARG;
+    // (rows of different lengths: in place would be other rows' place)
+    const int64_t in = 4 * B * h->n_leaves, out = 4 * B * h->n_nodes;
+    if (overlap(dlogits, out, mixture, in) || overlap(dlogits, out, dmixture, in)) return FFF_ERR_INVALID_ARG;
     DeviceGuard g(h->device);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     int n = 0;
@@ -2390,9 +2398,9 @@ fff_status_t fff_quantize_mx4(const void* src, fff_dtype_t dtype, int64_t rows, 
     fff_status_t s = check_mx4_args(dtype, rows, cols);
     if (s != FFF_OK || rows == 0 || cols == 0) return s;
     if (!src || !codes || !scales || !aligned16(src) || !aligned16(codes) || !aligned16(scales) || !aligned16(values)) return FFF_ERR_INVALID_ARG;
-    // (rows that start anywhere are read by vectors, of which a neighbour may have written its part)
-    const uintptr_t from = reinterpret_cast<uintptr_t>(src), to = reinterpret_cast<uintptr_t>(values), bytes = (uintptr_t)(rows * cols) * (dtype == FFF_DTYPE_F32 ? 4 : 2);
-    if (values && from < to + bytes && to < from + bytes) return FFF_ERR_INVALID_ARG;
+    // (a row's neighbours write theirs before it is read)
+    const int64_t bytes = rows * cols * (dtype == FFF_DTYPE_F32 ? 4 : 2), code_bytes = rows * ((cols + 1) / 2), scale_bytes = rows * ((cols + 31) / 32);
+    if (overlap(src, bytes, values, bytes) || overlap(src, bytes, codes, code_bytes) || overlap(src, bytes, scales, scale_bytes)) return FFF_ERR_INVALID_ARG;
     fff::LaunchOn on;
     if ((s = current_device(&on, cuda_stream)) != FFF_OK) return s;
     if (fff::quantize_mx4(on, src, dtype == FFF_DTYPE_F32 ? 4 : 2, rows, cols, codes, scales, values) != cudaSuccess)
@@ -2405,6 +2413,8 @@ fff_status_t fff_dequantize_mx4(const uint8_t* codes, const uint8_t* scales, fff
     fff_status_t s = check_mx4_args(dtype, rows, cols);
     if (s != FFF_OK || rows == 0 || cols == 0) return s;
     if (!codes || !scales || !values || !aligned16(codes) || !aligned16(scales) || !aligned16(values)) return FFF_ERR_INVALID_ARG;
+    const int64_t bytes = rows * cols * (dtype == FFF_DTYPE_F32 ? 4 : 2);
+    if (overlap(values, bytes, codes, rows * ((cols + 1) / 2)) || overlap(values, bytes, scales, rows * ((cols + 31) / 32))) return FFF_ERR_INVALID_ARG;
     fff::LaunchOn on;
     if ((s = current_device(&on, cuda_stream)) != FFF_OK) return s;
     if (fff::dequantize_mx4(on, codes, scales, dtype == FFF_DTYPE_F32 ? 4 : 2, rows, cols, values) != cudaSuccess)
