@@ -1553,7 +1553,9 @@ constexpr int64_t kTokenBlockMaxB = 512, kTokenBlockMaxBDeep = 2048, kTokenBlock
 // tokens 12.3 and 20.5, 500 20.5 and 21.2, 700 20.8 and 21.5, 1000 26.7 and 22.5; 1024 -> 1024, 2048 leaves of 32: 500 26.7 and 52.1, 1500
 // 49.2 and 61.5, 2000 61.5 and 70.5, 3000 86.0 and 77.8; 4096 leaves of 8: 2000 55.3 and 68.5, 3000 77.9 and 76.8; 512 -> 512, one leaf of
 // 32: 500 12.3 and 20.5, 1000 16.4 and 20.5, 1500 22.5 and 21.4.  A token expands all weights of its leaf for itself: wider leaves than
-// those count by their weights.
+// those count by their weights.  Wider leaves: 768 -> 768, 256 leaves of 64: 444 15.8 and 21.7, 592 22.1 and 21.7; of 96: 444 19.4 and 25.8, 592
+// 27.2 and 26.0; 2048 leaves of 64: 800 33.5 and 58.5, 1184 47.1 and 53.9; 256 -> 256, 2048 of 96: 1500 44.2 and 48.2, 2000 56.6 and 55.8;
+// 1024 -> 1024, 16 of 256: 200 32.1 and 53.1; one leaf of 512 -> 512, 256: 444 27.6 and 38.3; of 256 -> 256, 1024: 200 67.3 and 90.0.
 bool use_mx4_tokens(const fff_handle_s* h, int64_t B) {
     // (thin leaves: 1456 columns, 2048 leaves of one, 1964 tokens 57.3 and 46.1 with a warp per token)
     const int64_t most = (h->ustages.size() >= 2 ? (h->mx.mma ? 14 : 6) : h->depth == 0 ? 8 : 4) * (int64_t)h->sm_count;

@@ -104,7 +104,7 @@ constexpr float kGeluP0 = -0.9999930609869272f, kGeluP1 = 1.1512017022737409f, k
                 kGeluP3 = 0.05341210482228353f, kGeluP4 = 0.008080716673348184f, kGeluP5 = 0.0007692196373495289f,
                 kGeluP6 = 3.309279284094074e-05f;
 
-// The activations for kernels whose result is rounded to bf16 right away.
+// The activations for kernels whose result is rounded to bf16 right away, or (4-bit leaves) to a sum of two: GELU then keeps the error above.
 __device__ __forceinline__ float activate_bf16(int act, float v) {
     if (act == kActRelu) return fmaxf(v, 0.0f);
     if (act == kActGeluTanh) {

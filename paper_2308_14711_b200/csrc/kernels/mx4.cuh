@@ -761,8 +761,12 @@ k_mx4_copy_rows(uint16_t* __restrict__ dst, int dst_cols, const uint16_t* __rest
 // the next leaf's record is sent for to L2 at the same time.  The first product is split along D over the warps (MT = 2: over the two
 // groups of 16 hidden units too), so that no weight is expanded twice; the sums meet in shared memory, where bias and activation are
 // applied; for the second product every warp has output columns of its own.  Hidden values are kept as sums of two bf16 values (float32 precision to 2^-16):
-// the extra MMAs cost little next to the expansion.  Bound: latency and issue slots (42 % busy) with the 16 warps that 128 registers allow;
-// 1024 -> 1024, 2048 leaves of 32, 65 536 tokens 112 us, where its bytes take 46; more warps spill, fewer rows per tile expand weights twice.
+// the extra MMAs cost little next to the expansion.  Bound: latency and issue slots (42 % busy) with the 16 warps that 128 registers allow (leaves
+// of 17 to 32 spill 96 bytes there, the others 8); 1024 -> 1024, 2048 leaves of 32, 65 536 tokens 112 us, where its bytes take 46; more warps spill
+// more, fewer rows per tile expand weights twice.  The kernels that expand nothing are ahead: the whole forward takes 180 to 186 us there and 165
+// to 174 with bf16 weights, 66 and 61 to 63 on 768 -> 768, 256 leaves of 12, 50 432 tokens.
+// kWide, the latter with 48, 64 and 96 neurons per leaf: 102, 103 and 166 us (forward 124, 125 and 188; bf16 71, 76 and, on CUDA cores, 835);
+// 512 -> 512, 64 leaves of 256: 258 us (290; 1239).
 // MT: groups of 16 hidden units at a time: 1 for leaves of up to 16 (one K-block of 16 in the second product), else 2.
 // kWide: more than 32 hidden units: several passes over x, several K-blocks in the second product.
 template <int MT, bool kWide, bool kBig>
@@ -996,8 +1000,9 @@ struct MxTokenSmem {
 };
 
 // As k_token_block: a CTA walks one token down the tree and evaluates its leaf, with the arithmetic of k_leaf_mx4 on one token (its row
-// is every column of the MMAs' operand; what the other seven columns give is not stored).  Three CTAs per SM (80 registers, a few
-// spilled): two are 2 us ahead up to two per SM and a fifth behind from then on, four behind everywhere.
+// is every column of the MMAs' operand; what the other seven columns give is not stored).  Three CTAs per SM (80 registers; 8 bytes
+// spilled for leaves of up to 16, 24 of up to 32, 144 of wider ones): two are 2 us ahead up to two per SM and a fifth behind from then on, four behind
+// everywhere.
 template <int MT, bool kWide, bool kBig>
 __global__ void __launch_bounds__(kTBThreads, 3)
 k_mx4_token(const MxTokenArgs A)

@@ -11,8 +11,8 @@
 // which needs no logits: one pass over the mixture weights, bottom-up.
 //
 // All three are bound by HBM: 4 B L bytes are read (twice that with a second gradient) or written, a few operations each.  Of 6551 GB/s:
-// loss, 65 536 tokens of 2048 leaves 84.4 us (97 %); its gradient, 16 411 of 2048 24.5 us (84 %); back to the logits, 50 432 tokens of 256
-// leaves 28.4 us (82 %), where issue slots count as well: some 25 instructions per node.
+// loss, 65 536 tokens of 2048 leaves 84.4 to 86 us (95 to 97 %); its gradient, 16 411 of 2048 24.5 us (84 %); back to the logits, 50 432
+// tokens of 256 leaves 28.4 to 29 us (80 to 82 %), where issue slots count as well: some 25 instructions per node.
 #pragma once
 
 #include <float.h>
@@ -59,7 +59,8 @@ enum : int { kBalFew = 0, kBalMany = 1, kBalRows = 2 };
 // Grid (slices, tiles).  Every CTA adds up its rows of its columns and counts its rows' leaves among them; the last CTA of a tile
 // adds up the slices in their order, the last tile the tiles: one launch, and the same bits every time.
 // V: columns per thread (4; 1 for one or two leaves).  kHow: see above.  Rows are added in float32, 256 of a thread's at a time and then those sums (n rows: at
-// most 256 + n / 256 roundings); slices in float64.
+// most 256 + n / 256 roundings), then the threads of a column (at most 25 more); slices in float64.  (64 registers for two CTAs per SM; the
+// form for 64 leaves spills 32 bytes.)
 template <int V, int kHow>
 __global__ void __launch_bounds__(kBalThreads, 2)
 k_balance_loss(const float* __restrict__ mix, const int32_t* __restrict__ leaf_idx, const uint8_t* __restrict__ mask,
@@ -566,7 +567,7 @@ __device__ __forceinline__ void route_high(const float (&m)[kRouteU], const floa
     }
 }
 
-// kUp: dmixture given; kBal: counts and dloss given (slope_table for more than kRouteMaxStagedLeaves leaves).
+// kUp: dmixture given; kBal: counts and dloss given (slope_table for more than kRouteMaxSlopeLeaves leaves).
 // Gradients are stored as they come: a row has 2^d - 1 of them and starts anywhere, a level's are next to each other, L2 puts them
 // together.  (Collected in shared memory, and stored as aligned vectors: the same times, 5 % more at 2048 leaves.)
 template <bool kUp, bool kBal, int D>

@@ -10,7 +10,8 @@ namespace fff {
 struct LaunchOn {
     cudaStream_t stream;
     int device, sm_count;
-    bool dependent;               // as a programmatic dependent launch: every kernel waits (pdl_wait) before its first global access
+    bool dependent;               // as a programmatic dependent launch: every kernel waits (pdl_wait) before its first access to anything that
+                                  // a kernel may have written (the weights of a handle are never written again, and may be read before)
 };
 
 template <typename... KArgs, typename... Args>
