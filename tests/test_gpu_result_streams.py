@@ -134,3 +134,32 @@ def test_other_kinds_of_streams(call):
         assert torch.equal(y, y2) and torch.equal(leaf, leaf2)
         assert all(torch.equal(a, b) for a, b in zip(codes, binding.quantize_mx4(x, want_values=True)))
     layer.close()
+
+
+def test_a_captured_call_on_a_stream_of_the_capture(call):
+    """A fork and a join within a capture: results of the forked call are memory of the graph, and every replay writes them."""
+    layer = make()
+    x = torch.randn(B, D, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    want = [t.clone() for t in layer.forward_infer(x)] + [t.clone() for t in binding.quantize_mx4(x, want_values=True)]
+    other = torch.randn(B, D, generator=torch.Generator().manual_seed(2)).bfloat16().cuda()
+    want_other = [t.clone() for t in layer.forward_infer(other)] + [t.clone() for t in binding.quantize_mx4(other, want_values=True)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        y, leaf = layer.forward_infer(x, stream=side)
+        layer.forward_infer(x, stream=side)                # (dropped at once)
+        q = binding.quantize_mx4(x, want_values=True, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((y, leaf) + tuple(q), want))
+    keep = x.clone()
+    x.copy_(other)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((y, leaf) + tuple(q), want_other))
+    x.copy_(keep)
+    del graph
+    layer.close()
