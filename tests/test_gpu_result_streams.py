@@ -69,7 +69,7 @@ def apart(a, b):
 
 @pytest.mark.parametrize("name", NAMES)
 def test_memory_of_results(call, name):
-    """By their addresses alone: nothing here reads or writes memory of two owners, whatever the allocator does."""
+    """By their addresses alone.  (A host so slow that the waiting stream is done by the time of a comparison shows nothing there.)"""
     run = calls()[name]
     side, main = torch.cuda.Stream(), torch.cuda.current_stream()
     torch.cuda.synchronize()
@@ -86,7 +86,7 @@ def test_memory_of_results(call, name):
     freed = places(old)
     del old
     got = [t for t in run(side) if t is not None]
-    assert not main.query() and apart(places(got), freed)
+    assert apart(places(got), freed) or main.query()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, expected))
     del got
@@ -98,7 +98,7 @@ def test_memory_of_results(call, name):
     there = places(got)
     del got
     new = again()
-    assert not side.query() and apart(places(new), there)
+    assert apart(places(new), there) or side.query()
     torch.cuda.synchronize()
     del new
     # dropped while the current stream has still to read them: the next call's results lie elsewhere
@@ -109,7 +109,7 @@ def test_memory_of_results(call, name):
     there = places(got)
     del got
     got = [t for t in run(side) if t is not None]
-    assert not main.query() and apart(places(got), there)
+    assert apart(places(got), there) or main.query()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(read, expected, got))
 
